@@ -383,6 +383,72 @@ galore_status galore_adafactor_refresh(const galore_hparams* hp, const galore_te
 galore_status galore_adafactor(const galore_tensor* R, const galore_tensor* M, const galore_tensor* row, const galore_tensor* col,
                                const galore_tensor* N, float beta1, int64_t k, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- AdamW over a list of tensors, gradient norm, clipping ----
+ * What a training program needs beside galore_step: the step of the parameters GaLore leaves alone (embeddings, output
+ * head, norm weights; or a whole stack at full rank, the baseline the paper compares with), and gradient clipping over
+ * all of them.  No context; nothing is allocated, and everything may be captured into a HIP graph (a replay repeats the
+ * call with the same lr and k).  All tensors are BORROWED device memory; a vector is a matrix of one row.  Lists of any
+ * length; count == 0 is valid.  Errors as for the other context-free calls (galore_last_error(NULL)).
+ *
+ * What galore_grad_norm writes, in DEVICE memory, 16-byte aligned: the calls after it on the stream read it there, no
+ * host wait in between. */
+typedef struct {
+  float norm;      /* |grad_scale| * sqrt(sum of the squares of all entries) */
+  float scale;     /* grad_scale * min(1, max_norm / (norm + 1e-6)); 0 if an entry is not finite */
+  float finite;    /* 1 if every entry of every gradient is finite, else 0 */
+  float reserved;
+} galore_grad_stats;
+
+/* Optimizer state of one weight.
+ *   m, v             : fp32 with W's shape, ld == cols, 16-byte aligned; or both GALORE_U8 codes in the format of
+ *                      galore_state, with blocks of 256 consecutive elements of the whole row-major tensor, the last one
+ *                      shorter where the tensor's size is no multiple of 256 (any shape; for rows of a multiple of 256
+ *                      elements these are the blocks of galore_state).
+ *   m_scale, v_scale : with 8-bit moments, fp32, ceil(rows * cols / 256) scales in any dense shape.  Else ignored.
+ *   master           : fp32 with W's shape, ld == cols, 16-byte aligned, for a bf16 W: the weight in full precision.  The
+ *                      step updates it and writes its rounding to W, whose old contents are not read.  data == NULL: none.
+ *   weight_decay     : decoupled, multiplies lr; per tensor, since norm weights usually have none.
+ * The caller clears m, v (and the scales) before the first step and sets master to the weight. */
+typedef struct {
+  galore_tensor m;
+  galore_tensor v;
+  galore_tensor m_scale;
+  galore_tensor v_scale;
+  galore_tensor master;
+  float weight_decay;
+} galore_adamw_state;
+
+/* One AdamW step of tensors W[0..count-1] with gradients G[i] of W[i]'s shape (fp32 or bf16, independent of W's type; any
+ * ld, any element alignment).  k >= 1 is the 1-based step of the bias correction.  With g = stats->scale * G (stats NULL:
+ * g = G):
+ *     m <- beta1 m + (1-beta1) g ;  v <- beta2 v + (1-beta2) g^2
+ *     W <- (1 - lr*weight_decay) W - lr (m / (1-beta1^k)) / (sqrt(v / (1-beta2^k)) + eps)
+ * in fp32, W rounded once.  If stats->finite is not 1 the call leaves every tensor as it was (k is the caller's: repeat it
+ * for the next step).  Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their
+ * block) non-finite.
+ * One launch for up to 56 tensors with fp32 moments, or up to 44 with 8-bit ones.
+ * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address; written
+ * tensors that overlap otherwise are not detected and must not be passed. */
+galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count,
+                           float beta1, float beta2, float eps, float lr, int64_t k, const galore_grad_stats* stats,
+                           void* hip_stream);
+
+/* Bytes of device workspace (256-byte aligned) galore_grad_norm needs for a list of `count` gradients. */
+galore_status galore_grad_norm_workspace_bytes(int32_t count, size_t* out_bytes);
+
+/* stats <- norm, clip factor and finiteness of a list of gradients, taken together (formulas at galore_grad_stats).
+ * grad_scale undoes a loss scale or averages accumulated gradients (1: neither); max_norm > 0, infinity for no clipping.
+ * Squares are added in 64 bits.  The workspace is the call's own until it has run: calls that overlap in time need one
+ * each. */
+galore_status galore_grad_norm(const galore_tensor* G, int32_t count, float grad_scale, float max_norm,
+                               galore_grad_stats* stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* G[i] <- stats->scale * G[i] in place, rounded once to G's type: clipping for gradients that galore_step (or anything
+ * else that takes plain gradients) reads.  Nothing is written where the factor is 1.  If stats->finite is not 1, G becomes
+ * zero; a program that wants such steps left out entirely reads `finite` on the host first.
+ * GALORE_ERR_INVALID_ARG if two tensors start at the same address. */
+galore_status galore_scale_grads(const galore_tensor* G, int32_t count, const galore_grad_stats* stats, void* hip_stream);
+
 /* ---- Instrumentation (measurement only, no part of the method) ----
  * Between galore_profile_start and galore_profile_stop every kernel group that galore_step or
  * galore_refresh_subspace enqueues is bracketed by a pair of HIP events on the context's

@@ -37,6 +37,15 @@ class galore_adafactor_state(ctypes.Structure):
     _fields_ = [("proj", galore_tensor), ("m", galore_tensor), ("row", galore_tensor), ("col", galore_tensor)]
 
 
+class galore_grad_stats(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_float), ("scale", ctypes.c_float), ("finite", ctypes.c_float), ("reserved", ctypes.c_float)]
+
+
+class galore_adamw_state(ctypes.Structure):
+    _fields_ = [("m", galore_tensor), ("v", galore_tensor), ("m_scale", galore_tensor), ("v_scale", galore_tensor),
+                ("master", galore_tensor), ("weight_decay", ctypes.c_float)]
+
+
 class galore_hparams(ctypes.Structure):
     _fields_ = [("rank", ctypes.c_int32), ("update_gap", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
@@ -56,7 +65,8 @@ EXPORTS = ["galore_status_string", "galore_workspace_bytes", "galore_init", "gal
            "galore_profile_start", "galore_profile_stop", "galore_set_concurrency",
            "galore_set_call_overlap", "galore_set_fused_adam", "galore_join", "galore_get_stream",
            "galore_two_sided_workspace_bytes", "galore_two_sided_step", "galore_two_sided_refresh",
-           "galore_adafactor_workspace_bytes", "galore_adafactor_step", "galore_adafactor_refresh", "galore_adafactor"]
+           "galore_adafactor_workspace_bytes", "galore_adafactor_step", "galore_adafactor_refresh", "galore_adafactor",
+           "galore_adamw", "galore_grad_norm_workspace_bytes", "galore_grad_norm", "galore_scale_grads"]
 STAGES = ["project_left", "project_right", "adam", "back", "transpose", "refresh"]
 
 _lib = None
@@ -103,6 +113,11 @@ def lib():
         L.galore_adafactor_step.argtypes = [hp, tp, tp, afp, i64, f32, vp, ctypes.c_size_t, vp]
         L.galore_adafactor_refresh.argtypes = [hp, tp, afp, vp, ctypes.c_size_t, vp]
         L.galore_adafactor.argtypes = [tp, tp, tp, tp, tp, f32, i64, vp, ctypes.c_size_t, vp]
+        asp = ctypes.POINTER(galore_adamw_state)
+        L.galore_adamw.argtypes = [tp, tp, asp, i32, f32, f32, f32, f32, i64, vp, vp]
+        L.galore_grad_norm_workspace_bytes.argtypes = [i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.galore_grad_norm.argtypes = [tp, i32, f32, f32, vp, vp, ctypes.c_size_t, vp]
+        L.galore_scale_grads.argtypes = [tp, i32, vp, vp]
         L.galore_profile_start.argtypes = [vp]
         L.galore_profile_stop.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
         _lib = L
@@ -121,6 +136,22 @@ def desc(t):
         raise ValueError("need a 2-D row-major tensor")
     return galore_tensor(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]),
                          _DTYPES[t.dtype])
+
+
+def param_desc(t):
+    """galore_tensor view of a parameter or gradient of any rank on the current device: a vector is one row, and the
+    trailing dimensions of a contiguous tensor of rank 3 and more are one."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("need a tensor on the current device")
+    if t.dim() < 2:
+        if t.dim() == 1 and t.shape[0] > 1 and t.stride(0) != 1:
+            raise ValueError("need a contiguous vector")
+        return galore_tensor(t.data_ptr(), 1, t.numel(), t.numel(), _DTYPES[t.dtype])
+    if t.dim() > 2:
+        if not t.is_contiguous():
+            raise ValueError("need a contiguous tensor")
+        return galore_tensor(t.data_ptr(), t.shape[0], t.numel() // max(t.shape[0], 1), t.numel() // max(t.shape[0], 1), _DTYPES[t.dtype])
+    return desc(t)
 
 
 def shape_desc(rows, cols, dtype, ld=None, data=None):
@@ -341,6 +372,123 @@ class GaLoreAdafactor:
 
     def step(self, weight, grad, lr):
         galore_adafactor_step(self.hp, weight, grad, self.state(), self.t, lr, self.workspace)
+        self.t += 1
+
+
+def _param_array(items):
+    """A list of tensors as descriptors; an array made by tensor_array as it is."""
+    if isinstance(items, ctypes.Array):
+        return items
+    return tensor_array(param_desc(t) for t in items)
+
+
+def _stats_ptr(stats):
+    if stats is None:
+        return None
+    if not stats.is_cuda or stats.device.index != torch.cuda.current_device() or stats.dtype != torch.float32 \
+            or stats.numel() != 4 or not stats.is_contiguous():
+        raise ValueError("stats: four contiguous fp32 numbers on the current device")
+    return stats.data_ptr()
+
+
+def galore_adamw(W, G, states, beta1, beta2, eps, lr, k, stats=None):
+    """W, G: lists of tensors or arrays of descriptors; states: list or array of galore_adamw_state."""
+    W, G, S = _param_array(W), _param_array(G), _arr(states, galore_adamw_state)
+    if not len(W) == len(G) == len(S):
+        raise ValueError("weights, gradients and states differ in number")
+    _check(lib().galore_adamw(W, G, S, len(W), beta1, beta2, eps, lr, int(k), _stats_ptr(stats), _stream()))
+
+
+def galore_grad_norm_workspace_bytes(count):
+    out = ctypes.c_size_t(0)
+    _check(lib().galore_grad_norm_workspace_bytes(count, ctypes.byref(out)))
+    return out.value
+
+
+def galore_grad_norm(G, grad_scale, max_norm, stats, workspace):
+    G = _param_array(G)
+    _check(lib().galore_grad_norm(G, len(G), grad_scale, max_norm, _stats_ptr(stats), workspace.data_ptr(), workspace.numel(), _stream()))
+
+
+def galore_scale_grads(G, stats):
+    G = _param_array(G)
+    _check(lib().galore_scale_grads(G, len(G), _stats_ptr(stats), _stream()))
+
+
+class GaLoreGradNorm:
+    """Norm and clip factor of a list of at most `count` gradients: owns the workspace and the four numbers on the device
+    (`stats`: norm, factor, 1 if all entries are finite, 0), which `GaLoreAdamW.step` and `scale` read there."""
+
+    def __init__(self, count, max_norm=float("inf"), device="cuda"):
+        self.max_norm = max_norm
+        self.workspace = torch.empty(galore_grad_norm_workspace_bytes(count), dtype=torch.uint8, device=device)
+        self.stats = torch.zeros(4, dtype=torch.float32, device=device)
+
+    def measure(self, grads, grad_scale=1.0):
+        """grads: tensors, or an array of their descriptors (tensor_array(param_desc(g) for g in ...))."""
+        galore_grad_norm(grads, grad_scale, self.max_norm, self.stats, self.workspace)
+        return self.stats
+
+    def scale(self, grads, stats=None):
+        """The gradients times the factor, in place: what galore_step needs, which takes plain gradients."""
+        galore_scale_grads(grads, self.stats if stats is None else stats)
+
+    def clip(self, grads, grad_scale=1.0):
+        grads = _param_array(grads)
+        self.measure(grads, grad_scale)
+        self.scale(grads)
+        return self.stats
+
+
+class GaLoreAdamW:
+    """AdamW for a list of parameters that GaLore leaves alone (any rank; embeddings, norm weights, biases): owns their
+    moments and, with master=True, fp32 master copies of the bf16 ones (torch memory, one flat buffer per kind), and
+    keeps the step count; all arithmetic happens in the library."""
+
+    _ALIGN = 256  # elements: the states of every tensor start at a multiple (16-byte alignment, blocks of the 8-bit format)
+
+    def __init__(self, weights, moments="f32", master=False, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, device="cuda"):
+        """moments: "f32" or "q8" (8-bit codes, one fp32 scale per 256 elements).  weight_decay: a number, or one per tensor."""
+        if moments not in ("f32", "q8"):
+            raise ValueError("moments: f32 or q8")
+        self.moments, self.beta1, self.beta2, self.eps, self.t = moments, beta1, beta2, eps, 0
+        weights = list(weights)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(weights)
+        if len(decay) != len(weights):
+            raise ValueError("one weight_decay per tensor")
+        for w in weights:
+            param_desc(w)  # refuses what a step could not take
+        starts, total = [], 0
+        for w in weights:
+            starts.append(total)
+            total += -(-w.numel() // self._ALIGN) * self._ALIGN
+        q8 = moments == "q8"
+        code = torch.uint8 if q8 else torch.float32
+        self.M_flat, self.V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
+        self.M_scale_flat, self.V_scale_flat = ((torch.zeros(total // self._ALIGN, device=device) for _ in range(2)) if q8 else (None, None))
+        self.master_flat = torch.zeros(total, device=device) if master else None
+        cut = lambda flat: [flat[s:s + w.numel()].view(w.shape) for s, w in zip(starts, weights)]
+        blocks = lambda flat: [flat[s // self._ALIGN:-(-(s + w.numel()) // self._ALIGN)] for s, w in zip(starts, weights)]
+        self.M, self.V = cut(self.M_flat), cut(self.V_flat)
+        self.M_scale, self.V_scale = (blocks(self.M_scale_flat), blocks(self.V_scale_flat)) if q8 else ([], [])
+        self.master = [m if w.dtype == torch.bfloat16 else None for m, w in zip(cut(self.master_flat), weights)] if master else [None] * len(weights)
+        none = galore_tensor(None, 0, 0, 0, GALORE_F32)
+        states = []
+        for i, w in enumerate(weights):
+            if self.master[i] is not None:
+                self.master[i].copy_(w.detach())
+            d = param_desc(w)
+            like = lambda t: galore_tensor(t.data_ptr(), d.rows, d.cols, d.cols, _DTYPES[t.dtype])
+            states.append(galore_adamw_state(like(self.M[i]), like(self.V[i]), param_desc(self.M_scale[i]) if q8 else none,
+                                             param_desc(self.V_scale[i]) if q8 else none,
+                                             like(self.master[i]) if self.master[i] is not None else none, decay[i]))
+        self._states = (galore_adamw_state * len(states))(*states)
+
+    def step(self, weights, grads, lr, stats=None):
+        """weights, grads: tensors in the constructor's order, or arrays of their descriptors.  stats: the result of a
+        GaLoreGradNorm; its factor is applied to the gradients, and where an entry was not finite nothing changes (the
+        step is counted all the same: set `t` back to repeat it)."""
+        galore_adamw(weights, grads, self._states, self.beta1, self.beta2, self.eps, lr, self.t + 1, stats)
         self.t += 1
 
 

@@ -1,0 +1,88 @@
+// AdamW over a list of tensors (adamw.hip) and the norm and scaling of a list of gradients (grad_norm.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace galore {
+
+// What galore_grad_norm leaves on the device and the calls after it read.
+struct GradStats {
+  float norm, scale, finite, reserved;
+};
+
+// A kernel's arguments stay under 4 KiB: so many tensors per launch.
+constexpr int kAdamWTensors = 56;
+constexpr int kAdamWQ8Tensors = 44;
+constexpr int kGradTensors = 128;
+
+struct AdamWTensor {
+  void* W;
+  const void* G;
+  float* M;
+  float* V;
+  float* master;   // NULL: W is its own master
+  int64_t count;   // rows * cols
+  int32_t cols, ldw, ldg;
+  float keep;      // 1 - lr * weight decay
+};
+
+struct AdamWQ8Tensor {
+  void* W;
+  const void* G;
+  uint8_t* Mc;
+  uint8_t* Vc;
+  float* Ms;
+  float* Vs;
+  float* master;
+  int64_t count;
+  int32_t cols, ldw, ldg;
+  float keep;
+};
+
+struct AdamWCall {
+  const GradStats* stats;  // NULL: gradients as they are
+  float beta1, beta2, eps, lr;
+  float inv_c1, inv_c2;    // 1 / (1 - beta^k)
+  int32_t count;
+  int32_t span;            // elements per workgroup
+};
+
+template <class Tensor, int N> struct AdamWList {
+  AdamWCall call;
+  int32_t begin[N];        // first workgroup of a tensor in the launch
+  uint8_t types[N];        // bit 0: W is bf16, bit 1: G is bf16
+  Tensor t[N];
+};
+typedef AdamWList<AdamWTensor, kAdamWTensors> AdamWGroup;
+typedef AdamWList<AdamWQ8Tensor, kAdamWQ8Tensors> AdamWQ8Group;
+static_assert(sizeof(AdamWGroup) <= 4096 && sizeof(AdamWQ8Group) <= 4096, "kernel arguments");
+
+// The host fills everything but begin and span.
+hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream);
+hipError_t launch_adamw_q8(AdamWQ8Group& g, hipStream_t stream);
+
+struct GradTensor {
+  void* G;
+  int64_t count;
+  int32_t cols, ld;
+};
+
+struct GradGroup {
+  int32_t count;
+  int32_t span;
+  int32_t begin[kGradTensors];
+  uint8_t bf16[kGradTensors];
+  GradTensor t[kGradTensors];
+};
+static_assert(sizeof(GradGroup) <= 4000, "kernel arguments");
+
+// Partial sums of squares, one per workgroup: an upper bound for a list of `count` tensors.
+size_t grad_norm_partials(int32_t count);
+// lists: the whole list in groups of kGradTensors.  partials: grad_norm_partials(count) doubles.
+hipError_t launch_grad_norm(GradGroup* lists, int n_lists, float grad_scale, float max_norm, GradStats* stats, double* partials, hipStream_t stream);
+hipError_t launch_scale_grads(GradGroup& g, const GradStats* stats, hipStream_t stream);
+
+}  // namespace galore

@@ -1,0 +1,208 @@
+// AdamW over a list of tensors, the global norm of a list of gradients and their scaling, behind the C ABI: validation
+// of the whole list, then as few launches as the kernels' argument space allows.  No context, nothing allocated.
+#include "adamw.hpp"
+#include "api_internal.hpp"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+using namespace galore;
+using namespace galore::api;
+
+static_assert(sizeof(galore_grad_stats) == sizeof(GradStats), "the device's view of the statistics");
+
+namespace {
+
+constexpr int64_t kBlock = 256;   // elements under one scale of the 8-bit moments
+
+// No two of the addresses that a call writes may be the same (the same tensor twice in a list, one buffer for two states).
+galore_status check_distinct(std::vector<const void*>& starts) {
+  std::sort(starts.begin(), starts.end());
+  for (size_t i = 1; i < starts.size(); ++i)
+    if (starts[i] == starts[i - 1]) return fail(nullptr, GALORE_ERR_INVALID_ARG, "two tensors that the call writes start at the same address");
+  return GALORE_OK;
+}
+
+galore_status check_stats(const galore_grad_stats* stats) {
+  if (reinterpret_cast<uintptr_t>(stats) & 15) return fail(nullptr, GALORE_ERR_ALIGN, "stats must be 16-byte aligned");
+  return GALORE_OK;
+}
+
+// fp32 or U8 state of W's shape, dense and aligned
+galore_status check_moment(const galore_tensor& t, const char* what, int i, const galore_tensor& W, int32_t dtype) {
+  galore_status s = check_matrix(nullptr, t, what, i, true, true);
+  if (s) return s;
+  if (t.dtype != dtype) return fail(nullptr, GALORE_ERR_DTYPE, "%s[%d] has the wrong dtype", what, i);
+  if (t.rows != W.rows || t.cols != W.cols || t.ld != t.cols) return fail(nullptr, GALORE_ERR_STATE, "%s[%d] must be dense with W's shape", what, i);
+  if (reinterpret_cast<uintptr_t>(t.data) & 15) return fail(nullptr, GALORE_ERR_ALIGN, "%s[%d] must be 16-byte aligned", what, i);
+  return GALORE_OK;
+}
+
+galore_status check_scales(const galore_tensor& t, const char* what, int i, int64_t blocks) {
+  galore_status s = check_matrix(nullptr, t, what, i, true);
+  if (s) return s;
+  if (t.dtype != GALORE_F32) return fail(nullptr, GALORE_ERR_DTYPE, "%s[%d] must be fp32", what, i);
+  if (t.rows * t.cols != blocks || t.ld != t.cols)
+    return fail(nullptr, GALORE_ERR_STATE, "%s[%d] must hold %lld scales, dense", what, i, (long long)blocks);
+  if (reinterpret_cast<uintptr_t>(t.data) & 3) return fail(nullptr, GALORE_ERR_ALIGN, "%s[%d] must be 4-byte aligned", what, i);
+  return GALORE_OK;
+}
+
+galore_status check_element_alignment(const galore_tensor& t, const char* what, int i) {
+  if (reinterpret_cast<uintptr_t>(t.data) % (t.dtype == GALORE_F32 ? 4 : 2))
+    return fail(nullptr, GALORE_ERR_ALIGN, "%s[%d] must be aligned to its elements", what, i);
+  return GALORE_OK;
+}
+
+// A matrix of one row, or with rows that follow each other, is one run of elements.
+int32_t run_ld(const galore_tensor& t) { return (int32_t)(t.rows == 1 ? t.cols : t.ld); }
+
+galore_status fill_grads(const galore_tensor* G, int32_t count, std::vector<GradGroup>& lists) {
+  if (count < 0) return fail(nullptr, GALORE_ERR_INVALID_ARG, "count %d < 0", count);
+  if (count > 0 && !G) return fail(nullptr, GALORE_ERR_INVALID_ARG, "G is NULL");
+  lists.resize((size_t)(count + kGradTensors - 1) / kGradTensors);
+  for (int32_t i = 0; i < count; ++i) {
+    galore_status s = check_matrix(nullptr, G[i], "G", i, true);
+    if (s || (s = check_element_alignment(G[i], "G", i))) return s;
+    GradGroup& g = lists[(size_t)i / kGradTensors];
+    const int j = g.count++;
+    g.bf16[j] = G[i].dtype == GALORE_BF16;
+    g.t[j].G = G[i].data;
+    g.t[j].count = G[i].rows * G[i].cols;
+    g.t[j].cols = (int32_t)G[i].cols;
+    g.t[j].ld = run_ld(G[i]);
+  }
+  return GALORE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count, float beta1,
+                           float beta2, float eps, float lr, int64_t k, const galore_grad_stats* stats, void* hip_stream) try {
+  if (count < 0) return fail(nullptr, GALORE_ERR_INVALID_ARG, "count %d < 0", count);
+  if (count > 0 && (!W || !G || !S)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "W / G / S is NULL");
+  if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) || !(eps >= 0.f))
+    return fail(nullptr, GALORE_ERR_INVALID_ARG, "betas / eps out of range");
+  if (!std::isfinite(lr)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "lr is not finite");
+  if (k < 1) return fail(nullptr, GALORE_ERR_INVALID_ARG, "k must be >= 1");
+  galore_status s = check_stats(stats);
+  if (s) return s;
+  std::vector<const void*> written;
+  written.reserve((size_t)count * 6);
+  for (int32_t i = 0; i < count; ++i) {
+    const galore_adamw_state& st = S[i];
+    if ((s = check_matrix(nullptr, W[i], "W", i, true)) || (s = check_matrix(nullptr, G[i], "G", i, true)) ||
+        (s = check_element_alignment(W[i], "W", i)) || (s = check_element_alignment(G[i], "G", i)))
+      return s;
+    if (G[i].rows != W[i].rows || G[i].cols != W[i].cols) return fail(nullptr, GALORE_ERR_SHAPE, "G[%d] must have W's shape", i);
+    if (!(st.weight_decay >= 0.f)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "weight_decay of tensor %d out of range", i);
+    const bool q8 = st.m.dtype == GALORE_U8;
+    if ((s = check_moment(st.m, "m", i, W[i], q8 ? GALORE_U8 : GALORE_F32)) || (s = check_moment(st.v, "v", i, W[i], q8 ? GALORE_U8 : GALORE_F32)))
+      return s;
+    if (q8) {
+      const int64_t blocks = (W[i].rows * W[i].cols + kBlock - 1) / kBlock;
+      if ((s = check_scales(st.m_scale, "m_scale", i, blocks)) || (s = check_scales(st.v_scale, "v_scale", i, blocks))) return s;
+      written.push_back(st.m_scale.data);
+      written.push_back(st.v_scale.data);
+    }
+    if (st.master.data) {
+      if (W[i].dtype != GALORE_BF16) return fail(nullptr, GALORE_ERR_DTYPE, "master copies belong to bf16 weights (tensor %d)", i);
+      if ((s = check_moment(st.master, "master", i, W[i], GALORE_F32))) return s;
+      written.push_back(st.master.data);
+    }
+    written.push_back(W[i].data);
+    written.push_back(st.m.data);
+    written.push_back(st.v.data);
+  }
+  if ((s = check_distinct(written))) return s;
+
+  AdamWCall call{};
+  call.stats = reinterpret_cast<const GradStats*>(stats);
+  call.beta1 = beta1; call.beta2 = beta2; call.eps = eps; call.lr = lr;
+  call.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)k)));
+  call.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)beta2, (double)k)));
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  AdamWGroup g{};
+  AdamWQ8Group q{};
+  g.call = q.call = call;
+  const auto types = [&](int32_t i) { return (uint8_t)((W[i].dtype == GALORE_BF16 ? 1 : 0) | (G[i].dtype == GALORE_BF16 ? 2 : 0)); };
+  const auto common = [&](auto& t, int32_t i) {
+    t.W = W[i].data; t.G = G[i].data;
+    t.master = static_cast<float*>(S[i].master.data);
+    t.count = W[i].rows * W[i].cols;
+    t.cols = (int32_t)W[i].cols; t.ldw = run_ld(W[i]); t.ldg = run_ld(G[i]);
+    t.keep = (float)(1.0 - (double)lr * (double)S[i].weight_decay);
+  };
+  for (int32_t i = 0; i < count && e == hipSuccess; ++i) {
+    if (S[i].m.dtype == GALORE_U8) {
+      const int j = q.call.count++;
+      common(q.t[j], i);
+      q.types[j] = types(i);
+      q.t[j].Mc = static_cast<uint8_t*>(S[i].m.data); q.t[j].Vc = static_cast<uint8_t*>(S[i].v.data);
+      q.t[j].Ms = static_cast<float*>(S[i].m_scale.data); q.t[j].Vs = static_cast<float*>(S[i].v_scale.data);
+      if (q.call.count == kAdamWQ8Tensors) { e = launch_adamw_q8(q, stream); q.call.count = 0; }
+    } else {
+      const int j = g.call.count++;
+      common(g.t[j], i);
+      g.types[j] = types(i);
+      g.t[j].M = static_cast<float*>(S[i].m.data); g.t[j].V = static_cast<float*>(S[i].v.data);
+      if (g.call.count == kAdamWTensors) { e = launch_adamw(g, stream); g.call.count = 0; }
+    }
+  }
+  if (e == hipSuccess) e = launch_adamw(g, stream);
+  if (e == hipSuccess) e = launch_adamw_q8(q, stream);
+  return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "AdamW launch");
+} catch (...) {
+  return fail(nullptr, GALORE_ERR_INVALID_ARG, "out of host memory");
+}
+
+galore_status galore_grad_norm_workspace_bytes(int32_t count, size_t* out_bytes) {
+  if (count < 0 || !out_bytes) return fail(nullptr, GALORE_ERR_INVALID_ARG, "count < 0 or out_bytes is NULL");
+  *out_bytes = align_up(grad_norm_partials(count) * sizeof(double));
+  return GALORE_OK;
+}
+
+galore_status galore_grad_norm(const galore_tensor* G, int32_t count, float grad_scale, float max_norm, galore_grad_stats* stats,
+                               void* workspace, size_t workspace_bytes, void* hip_stream) try {
+  if (!stats) return fail(nullptr, GALORE_ERR_INVALID_ARG, "stats is NULL");
+  if (!std::isfinite(grad_scale)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "grad_scale is not finite");
+  if (!(max_norm > 0.f)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "max_norm must be > 0 (infinity: no clipping)");
+  galore_status s = check_stats(stats);
+  if (s) return s;
+  std::vector<GradGroup> lists;
+  if ((s = fill_grads(G, count, lists))) return s;
+  if (!workspace) return fail(nullptr, GALORE_ERR_WORKSPACE, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(nullptr, GALORE_ERR_ALIGN, "workspace must be 256-byte aligned");
+  const size_t need = grad_norm_partials(count) * sizeof(double);
+  if (workspace_bytes < need) return fail(nullptr, GALORE_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const hipError_t e = launch_grad_norm(lists.data(), (int)lists.size(), grad_scale, max_norm, reinterpret_cast<GradStats*>(stats),
+                                        static_cast<double*>(workspace), static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "gradient norm launch");
+} catch (...) {
+  return fail(nullptr, GALORE_ERR_INVALID_ARG, "out of host memory");
+}
+
+galore_status galore_scale_grads(const galore_tensor* G, int32_t count, const galore_grad_stats* stats, void* hip_stream) try {
+  if (!stats) return fail(nullptr, GALORE_ERR_INVALID_ARG, "stats is NULL");
+  galore_status s = check_stats(stats);
+  if (s) return s;
+  std::vector<GradGroup> lists;
+  if ((s = fill_grads(G, count, lists))) return s;
+  std::vector<const void*> written;
+  written.reserve((size_t)count);
+  for (int32_t i = 0; i < count; ++i) written.push_back(G[i].data);
+  if ((s = check_distinct(written))) return s;
+  hipError_t e = hipSuccess;
+  for (size_t l = 0; l < lists.size() && e == hipSuccess; ++l)
+    e = launch_scale_grads(lists[l], reinterpret_cast<const GradStats*>(stats), static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "gradient scaling launch");
+} catch (...) {
+  return fail(nullptr, GALORE_ERR_INVALID_ARG, "out of host memory");
+}
+
+}  // extern "C"

@@ -1,0 +1,67 @@
+// Launches over a whole list of tensors (adamw.hip, grad_norm.hip): the list is a kernel argument, every workgroup takes
+// one span of consecutive elements of one tensor.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace galore {
+
+constexpr int64_t kMaxBlocks = (int64_t)1 << 23;  // workgroups per launch: a launch has fewer than 2^32 work-items
+
+// Tensor that workgroup `block` belongs to: begin[i] is the first workgroup of tensor i, ascending.  One load per 64
+// tensors and a ballot in place of a binary search, whose steps would wait for each other.
+template <int N> __device__ __forceinline__ int tensor_of_block(const int32_t (&begin)[N], int count, int block) {
+  const int lane = threadIdx.x & 63;
+  int found = -1;
+#pragma unroll
+  for (int base = 0; base < N; base += 64) {
+    const int i = base + lane;
+    const int b = i < count && i < N ? begin[i < N ? i : 0] : INT32_MAX;
+    found += __popcll(__ballot(b <= block));
+  }
+  return __builtin_amdgcn_readfirstlane(found);
+}
+
+// Element o of a span that starts at (row, col) of a matrix with `cols` columns, as an offset from the matrix' first
+// element.  o < 2^20 and cols < 2^30: the division is one of 32 bits.
+struct RowWalk {
+  int64_t row;
+  uint32_t col, cols;
+  int64_t ld;
+  __device__ __forceinline__ RowWalk(int64_t first, int32_t cols_, int32_t ld_) : cols(cols_), ld(ld_) {
+    row = first / cols_;
+    col = (uint32_t)(first - row * cols_);
+  }
+  // offset of element o, and how many elements follow it in its row (itself included)
+  __device__ __forceinline__ int64_t at(int o, uint32_t& left) const {
+    const uint32_t c = col + (uint32_t)o, r = c / cols, x = c - r * cols;
+    left = cols - x;
+    return (row + r) * ld + x;
+  }
+};
+
+// Vectors at element alignment: the hardware takes global accesses at any alignment.
+typedef float list_f32x4 __attribute__((ext_vector_type(4)));
+typedef float list_f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 list_bf16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float list_f32x8_any __attribute__((ext_vector_type(8), aligned(4)));
+typedef __bf16 list_bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+template <class T, int N> struct ListVec;
+template <> struct ListVec<float, 4> { typedef list_f32x4_any type; };
+template <> struct ListVec<__bf16, 4> { typedef list_bf16x4_any type; };
+template <> struct ListVec<float, 8> { typedef list_f32x8_any type; };
+template <> struct ListVec<__bf16, 8> { typedef list_bf16x8_any type; };
+template <int N> using ListF32 = float __attribute__((ext_vector_type(N)));
+
+template <int N, class T> __device__ __forceinline__ ListF32<N> list_load(const T* p) {
+  typedef typename ListVec<T, N>::type V;
+  return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const V*>(p)), ListF32<N>);
+}
+template <int N, class T> __device__ __forceinline__ void list_store(T* p, ListF32<N> x) {
+  typedef typename ListVec<T, N>::type V;
+  __builtin_nontemporal_store(__builtin_convertvector(x, V), reinterpret_cast<V*>(p));
+}
+
+}  // namespace galore
