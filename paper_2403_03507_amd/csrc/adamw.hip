@@ -8,13 +8,17 @@
 // adam_q8.hip, with blocks of 256 consecutive elements of the whole tensor.
 #include "adamw.hpp"
 
+#include <type_traits>
+
 #include "adam_entry.hpp"
 #include "tensor_list.hpp"
 
 namespace galore {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kSpan = 512;      // elements per workgroup: one group of 4 per thread
+constexpr int kSpanQ8 = 1024;   // 8 per thread
 
 struct Scalars {
   float scale, beta1, beta2, eps, lr, inv_c1, inv_c2, keep;
@@ -27,12 +31,26 @@ __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { ret
 template <class TW, class TG, bool MASTER>
 __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& s, int64_t first, int n) {
   typedef ListF32<4> f4;
+  const int o = threadIdx.x * 4;
+  if (o >= n) return;
   float* __restrict__ M = p.M + first;
   float* __restrict__ V = p.V + first;
   float* __restrict__ X = MASTER ? p.master + first : nullptr;
   TW* __restrict__ W = static_cast<TW*>(p.W);
   const TG* __restrict__ G = static_cast<const TG*>(p.G);
-  const auto step4 = [&](f4 g, f4& m, f4& v, f4& w) {
+  int64_t aw = o, ag = o;
+  uint32_t left = 4;
+  const bool dense = p.ldw == p.cols && p.ldg == p.cols;
+  if (dense) {
+    W += first; G += first;
+  } else {
+    aw = RowWalk(first, p.cols, p.ldw).at(o, left);
+    ag = RowWalk(first, p.cols, p.ldg).at(o, left);
+  }
+  if (o + 4 <= n && left >= 4) {
+    const f4 g = list_load<4>(G + ag);
+    f4 m = list_load<4>(M + o), v = list_load<4>(V + o);
+    f4 w = MASTER ? list_load<4>(X + o) : list_load<4>(W + aw);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float me = m[e], ve = v[e];
@@ -40,50 +58,23 @@ __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& 
       m[e] = me; v[e] = ve;
       w[e] = apply(w[e], ne, s);
     }
-  };
-  const auto one = [&](int o, int64_t aw, int64_t ag) {
-    float m = M[o], v = V[o];
-    const float ne = adam_entry(s.scale * (float)G[ag], m, v, s.beta1, s.beta2, s.eps, s.inv_c1, s.inv_c2);
-    M[o] = m; V[o] = v;
-    const float w = apply(MASTER ? X[o] : (float)W[aw], ne, s);
-    if (MASTER) X[o] = w;
-    W[aw] = (TW)w;
-  };
-  const bool dense = p.ldw == p.cols && p.ldg == p.cols;
-  if (dense) {
-    W += first; G += first;
-    for (int o = threadIdx.x * 4; o < n; o += kThreads * 4) {
-      if (o + 4 <= n) {
-        const f4 g = list_load<4>(G + o);
-        f4 m = list_load<4>(M + o), v = list_load<4>(V + o);
-        f4 w = MASTER ? list_load<4>(X + o) : list_load<4>(W + o);
-        step4(g, m, v, w);
-        list_store<4>(M + o, m);
-        list_store<4>(V + o, v);
-        if (MASTER) list_store<4>(X + o, w);
-        list_store<4>(W + o, w);
-      } else {
-        for (int e = o; e < n; ++e) one(e, e, e);
-      }
-    }
+    list_store<4>(M + o, m);
+    list_store<4>(V + o, v);
+    if (MASTER) list_store<4>(X + o, w);
+    list_store<4>(W + aw, w);
     return;
   }
-  const RowWalk walk_w(first, p.cols, p.ldw), walk_g(first, p.cols, p.ldg);
-  for (int o = threadIdx.x * 4; o < n; o += kThreads * 4) {
-    uint32_t left;
-    const int64_t aw = walk_w.at(o, left), ag = walk_g.at(o, left);
-    if (o + 4 <= n && left >= 4) {
-      const f4 g = list_load<4>(G + ag);
-      f4 m = list_load<4>(M + o), v = list_load<4>(V + o);
-      f4 w = MASTER ? list_load<4>(X + o) : list_load<4>(W + aw);
-      step4(g, m, v, w);
-      list_store<4>(M + o, m);
-      list_store<4>(V + o, v);
-      if (MASTER) list_store<4>(X + o, w);
-      list_store<4>(W + aw, w);
-    } else {
-      for (int e = o; e < o + 4 && e < n; ++e) one(e, walk_w.at(e, left), walk_g.at(e, left));
-    }
+  // the end of the tensor, or of a row with a gap behind it
+  const RowWalk walk_w(dense ? 0 : first, p.cols, p.ldw), walk_g(dense ? 0 : first, p.cols, p.ldg);
+#pragma unroll 1
+  for (int e = o; e < o + 4 && e < n; ++e) {
+    const int64_t we = dense ? e : walk_w.at(e, left), ge = dense ? e : walk_g.at(e, left);
+    float m = M[e], v = V[e];
+    const float ne = adam_entry(s.scale * (float)G[ge], m, v, s.beta1, s.beta2, s.eps, s.inv_c1, s.inv_c2);
+    M[e] = m; V[e] = v;
+    const float w = apply(MASTER ? X[e] : (float)W[we], ne, s);
+    if (MASTER) X[e] = w;
+    W[we] = (TW)w;
   }
 }
 
@@ -93,11 +84,12 @@ __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup g
     if (grp.call.stats->finite != 1.f) return;  // the whole step is left out
     s.scale = grp.call.stats->scale;
   }
-  const int i = tensor_of_block(grp.begin, grp.call.count, blockIdx.x);
+  const int block = grp.call.block0 + span_of_block();
+  const int i = tensor_of_block(grp.begin, grp.call.count, block);
   const AdamWTensor& p = grp.t[i];
   s.keep = p.keep;
-  const int64_t first = (int64_t)(blockIdx.x - grp.begin[i]) * grp.call.span, rest = p.count - first;
-  const int n = rest < grp.call.span ? (int)rest : grp.call.span;
+  const int64_t first = (int64_t)(block - grp.begin[i]) * kSpan, rest = p.count - first;
+  const int n = rest < kSpan ? (int)rest : kSpan;
   const bool master = p.master != nullptr;
   switch (grp.types[i]) {
     case 0: adamw_span<float, float, false>(p, s, first, n); break;
@@ -113,8 +105,15 @@ __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup g
 }
 
 // ---- 8-bit moments -----------------------------------------------------------------------------------
+// Half a wavefront owns a block of 256 elements, 8 to a lane.  With 10 bytes to move per bf16 element the arithmetic counts
+// as much as the traffic: 64 additions or the like per element would take as long as the bytes do.  So first-moment codes
+// go through the hardware's e4m3 conversions, second-moment codes are cut from fp32 bits, and the square root and the
+// reciprocal of the update are the hardware's approximations of one unit in the last place (exact ones: 202M bf16 elements
+// 420 us instead of 348).
 
 typedef float q_f32x2 __attribute__((ext_vector_type(2)));
+typedef short q_s16x2 __attribute__((ext_vector_type(2)));
+constexpr int kBlock = 256, kLanes = 32;
 
 // Maximum over the 32 lanes that hold one block, every lane gets it; NaN if one of them is NaN.
 __device__ __forceinline__ float block_max(float x) {
@@ -126,36 +125,40 @@ __device__ __forceinline__ float block_max(float x) {
   x = __builtin_elementwise_maximum(x, dpp(x, integral_constant<int, 0xB1>{}));    // quad_perm [1,0,3,2]
   x = __builtin_elementwise_maximum(x, dpp(x, integral_constant<int, 0x4E>{}));    // quad_perm [2,3,0,1]
   x = __builtin_elementwise_maximum(x, dpp(x, integral_constant<int, 0x141>{}));   // row_half_mirror
-  x = __builtin_elementwise_maximum(x, dpp(x, integral_constant<int, 0x140>{}));   // row_mirror
-  const int y = __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x401F);   // the lane 16 away
+  x = __builtin_elementwise_maximum(x, dpp(x, integral_constant<int, 0x140>{}));   // row_mirror: each row of 16 holds its maximum
+  const int y = __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x401F);   // the lane 16 away, of the same 32
   return __builtin_elementwise_maximum(x, __builtin_bit_cast(float, y));
 }
 
 // First-moment codes are OCP e4m3 numbers, 256 times the magnitude: the hardware's conversions decode and encode them
-// (round to nearest even, subnormals included).
+// (round to nearest even, subnormals included) and take the factor 2^-8 along.
 __device__ __forceinline__ void decode_m4(uint32_t c, float scale, float* m) {
-  const q_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-  m[0] = a[0] * 0x1p-8f * scale; m[1] = a[1] * 0x1p-8f * scale;
-  m[2] = b[0] * 0x1p-8f * scale; m[3] = b[1] * 0x1p-8f * scale;
+  const q_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 0x1p-8f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 0x1p-8f, true);
+  m[0] = a[0] * scale; m[1] = a[1] * scale; m[2] = b[0] * scale; m[3] = b[1] * scale;
 }
 __device__ __forceinline__ uint32_t encode_m4(const float* m, float inverse) {
-  float y[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_fmed3f(m[e] * inverse, -1.f, 1.f) * 256.f;
-  int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+  q_s16x2 c{0, 0};
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, m[0] * inverse, m[1] * inverse, 0x1p-8f, false);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, m[2] * inverse, m[3] * inverse, 0x1p-8f, true);
+  return __builtin_bit_cast(uint32_t, c);
 }
 // Second-moment codes (5 exponent bits from 2^-30, 3 mantissa bits, no sign) are the bits of an fp32 number from bit 20
 // on, 2^96 too small; its subnormals are the codes' own.
 __device__ __forceinline__ void decode_v4(uint32_t c, float scale, float* v) {
+  const float k = 0x1p96f * scale;
+  if (scale < 0x1p31f) {  // k is finite: one exact factor
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(float, ((c >> (8 * e)) & 0xFFu) << 20) * 0x1p96f * scale;
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(float, ((c >> (8 * e)) & 0xFFu) << 20) * k;
+  } else {                // NaN comes here as well
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(float, ((c >> (8 * e)) & 0xFFu) << 20) * 0x1p96f * scale;
+  }
 }
 __device__ __forceinline__ uint32_t encode_v4(const float* v, float inverse) {
   uint32_t out = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float y = fminf(v[e] * inverse, 1.f);
+    const float y = v[e] * inverse;   // at most 1 and an ulp, which rounds to 1
     const uint32_t bits = __builtin_bit_cast(uint32_t, y);
     // nearest, ties to even, in 3 mantissa bits; below 2^-30 in steps of 2^-33, which an addition to 2^-10 rounds to
     const uint32_t normal = ((bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20) - (96u << 3);
@@ -165,90 +168,164 @@ __device__ __forceinline__ uint32_t encode_v4(const float* v, float inverse) {
   return out;
 }
 
-template <class TW, class TG, bool MASTER>
-__device__ __forceinline__ void adamw_q8_span(const AdamWQ8Tensor& p, const Scalars& s, int64_t first, int n) {
+// The step of one lane's 8 elements: g, w, and the codes of the block with scales sm, sv, in and out.
+__device__ __forceinline__ void step_q8(const ListF32<8>& g, ListF32<8>& w, uint32_t (&cm)[2], uint32_t (&cv)[2], float& sm, float& sv,
+                                        const Scalars& s) {
 #pragma clang fp contract(off)
-  typedef ListF32<8> f8;
-  uint8_t* __restrict__ Mc = p.Mc + first;
-  uint8_t* __restrict__ Vc = p.Vc + first;
-  float* __restrict__ Ms = p.Ms + (first >> 8);
-  float* __restrict__ Vs = p.Vs + (first >> 8);
-  float* __restrict__ X = MASTER ? p.master + first : nullptr;
-  TW* __restrict__ W = static_cast<TW*>(p.W);
-  const TG* __restrict__ G = static_cast<const TG*>(p.G);
-  const bool dense = p.ldw == p.cols && p.ldg == p.cols;
-  const RowWalk walk_w(first, p.cols, p.ldw), walk_g(first, p.cols, p.ldg);
-  if (dense) { W += first; G += first; }
-  const float omb1 = 1.f - s.beta1, omb2 = 1.f - s.beta2;
-  const int in_block = (threadIdx.x & 31) * 8;
-  for (int b = threadIdx.x >> 5; b * 256 < n; b += kThreads / 32) {  // the 32 lanes of a block stay together
-    const int o = b * 256 + in_block;
-    uint32_t left_w = 8, left_g = 8;
-    const int64_t aw = dense ? o : walk_w.at(o, left_w), ag = dense ? o : walk_g.at(o, left_g);
-    const bool whole = o + 8 <= n && left_w >= 8 && left_g >= 8;
-    uint2 cm{0, 0}, cv{0, 0};
-    f8 g = 0.f, w = 0.f;
-    if (whole) {
-      g = list_load<8>(G + ag);
-      cm = *reinterpret_cast<const uint2*>(Mc + o);
-      cv = *reinterpret_cast<const uint2*>(Vc + o);
-      w = MASTER ? list_load<8>(X + o) : list_load<8>(W + aw);
+  const float omb1 = 1.f - s.beta1, omb2 = 1.f - s.beta2, rate = -s.lr * s.inv_c1;
+  float m[8], v[8];
+  decode_m4(cm[0], sm, m); decode_m4(cm[1], sm, m + 4);
+  decode_v4(cv[0], sv, v); decode_v4(cv[1], sv, v + 4);
+  float amax = 0.f, vmax = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float ge = s.scale * g[e];
+    const float gm = omb1 * ge;
+    m[e] = __builtin_fmaf(s.beta1, m[e], gm);
+    float gv = omb2 * ge;
+    gv = gv * ge;
+    v[e] = __builtin_fmaf(s.beta2, v[e], gv);
+    // the approximations take no subnormal numbers: 1.1e-19 is the smallest square root (and 0 / 0 at eps = 0 is 0)
+    const float den = __builtin_amdgcn_sqrtf(fmaxf(v[e] * s.inv_c2, 0x1p-126f)) + s.eps;
+    w[e] = __builtin_fmaf(rate, m[e] * __builtin_amdgcn_rcpf(den), s.keep * w[e]);
+    amax = __builtin_elementwise_maximum(amax, __builtin_fabsf(m[e]));
+    vmax = __builtin_elementwise_maximum(vmax, v[e]);
+  }
+  sm = amax = block_max(amax);
+  sv = vmax = block_max(vmax);
+  float inv_m = amax != 0.f ? 1.f / amax : 0.f, inv_v = vmax != 0.f ? 1.f / vmax : 0.f;
+  // a scale below 2^-128 has no finite reciprocal: every entry but zero takes the largest code
+  if (inv_m > 0x1.fffffep127f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = m[e] == 0.f ? 0.f : __builtin_copysignf(1.f, m[e]);
+    inv_m = 1.f;
+  }
+  if (inv_v > 0x1.fffffep127f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v[e] == 0.f ? 0.f : 1.f;
+    inv_v = 1.f;
+  }
+  cm[0] = encode_m4(m, inv_m); cm[1] = encode_m4(m + 4, inv_m);
+  cv[0] = encode_v4(v, inv_v); cv[1] = encode_v4(v + 4, inv_v);
+}
+
+// One lane's share of a block: where its 8 elements are and what it needs to reach them.
+struct LaneQ8 {
+  int64_t first;       // the span's first element in the tensor
+  int at0, at1;        // the lane's two groups of 4 in the span
+  int n0, n1;          // how many of them the tensor has
+  bool simple;         // a whole block of a tensor without gaps between its rows
+};
+
+// Four elements from the o-th of a span on, `n` of them (the others count as zero): rows may lie apart.
+template <class T> __device__ __forceinline__ ListF32<4> load_group(const T* p, const RowWalk& walk, int o, int n) {
+  ListF32<4> x = 0.f;
+  if (n <= 0) return x;
+  uint32_t left;
+  const int64_t a = walk.at(o, left);
+  if (n >= 4 && left >= 4) return list_load<4>(p + a);
+  x[0] = (float)p[a];
+#pragma unroll
+  for (int e = 1; e < 4; ++e)
+    if (e < n) x[e] = (float)p[walk.at(o + e, left)];
+  return x;
+}
+template <class T> __device__ __forceinline__ void store_group(T* p, const RowWalk& walk, int o, int n, ListF32<4> x) {
+  if (n <= 0) return;
+  uint32_t left;
+  const int64_t a = walk.at(o, left);
+  if (n >= 4 && left >= 4) { list_store<4>(p + a, x); return; }
+  p[a] = (T)x[0];
+#pragma unroll
+  for (int e = 1; e < 4; ++e)
+    if (e < n) p[walk.at(o + e, left)] = (T)x[e];
+}
+
+template <class TW, class TG, bool MASTER, bool ROW>
+__device__ __forceinline__ void load_q8(const AdamWQ8Tensor& p, const LaneQ8& l, ListF32<8>& g, ListF32<8>& w) {
+  typedef typename std::conditional<MASTER, float, TW>::type TX;
+  const TX* X = MASTER ? reinterpret_cast<const TX*>(p.master) : static_cast<const TX*>(p.W);
+  const TG* G = static_cast<const TG*>(p.G);
+  ListF32<4> g0, g1, w0, w1;
+  if (l.simple) {
+    X += l.first; G += l.first;
+    if (ROW) {
+      g = list_load<8>(G + l.at0);
+      w = list_load<8>(X + l.at0);
+      return;
+    }
+    g0 = list_load<4>(G + l.at0); g1 = list_load<4>(G + l.at1);
+    w0 = list_load<4>(X + l.at0); w1 = list_load<4>(X + l.at1);
+  } else {
+    const RowWalk walk_w(l.first, p.cols, MASTER ? p.cols : p.ldw), walk_g(l.first, p.cols, p.ldg);
+    g0 = load_group(G, walk_g, l.at0, l.n0); g1 = load_group(G, walk_g, l.at1, l.n1);
+    w0 = load_group(X, walk_w, l.at0, l.n0); w1 = load_group(X, walk_w, l.at1, l.n1);
+  }
+  g = __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7);
+  w = __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <class TW, bool MASTER, bool ROW>
+__device__ __forceinline__ void store_q8(const AdamWQ8Tensor& p, const LaneQ8& l, const ListF32<8>& w) {
+  TW* W = static_cast<TW*>(p.W);
+  const ListF32<4> w0 = __builtin_shufflevector(w, w, 0, 1, 2, 3), w1 = __builtin_shufflevector(w, w, 4, 5, 6, 7);
+  if (l.simple) {
+    W += l.first;
+    if (MASTER) {
+      float* X = p.master + l.first;
+      list_store<4>(X + l.at0, w0);
+      list_store<4>(X + l.at1, w1);
+    }
+    if (ROW) {
+      list_store<8>(W + l.at0, w);
     } else {
-      uint32_t lm[2] = {0, 0}, lv[2] = {0, 0};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (o + e < n) {
-          uint32_t left;
-          g[e] = (float)G[dense ? o + e : walk_g.at(o + e, left)];
-          w[e] = MASTER ? X[o + e] : (float)W[dense ? o + e : walk_w.at(o + e, left)];
-          lm[e >> 2] |= (uint32_t)Mc[o + e] << (8 * (e & 3));
-          lv[e >> 2] |= (uint32_t)Vc[o + e] << (8 * (e & 3));
-        }
-      }
-      cm = uint2{lm[0], lm[1]}; cv = uint2{lv[0], lv[1]};
+      list_store<4>(W + l.at0, w0);
+      list_store<4>(W + l.at1, w1);
     }
-    const float sm = Ms[b], sv = Vs[b];
-    float m[8], v[8];
-    decode_m4(cm.x, sm, m); decode_m4(cm.y, sm, m + 4);
-    decode_v4(cv.x, sv, v); decode_v4(cv.y, sv, v + 4);
-    float amax = 0.f, vmax = 0.f;
+    return;
+  }
+  if (MASTER) {
+    const RowWalk walk_x(l.first, p.cols, p.cols);
+    store_group(p.master, walk_x, l.at0, l.n0, w0);
+    store_group(p.master, walk_x, l.at1, l.n1, w1);
+  }
+  const RowWalk walk_w(l.first, p.cols, p.ldw);
+  store_group(W, walk_w, l.at0, l.n0, w0);
+  store_group(W, walk_w, l.at1, l.n1, w1);
+}
+
+typedef uint32_t q_u32x2 __attribute__((ext_vector_type(2)));
+
+// The codes of a lane's two groups; those of a tensor lie without gaps, so only the tensor's end is not whole.
+__device__ __forceinline__ uint32_t load_code4(const uint8_t* p, int n) {
+  if (n >= 4) return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+  uint32_t c = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float ge = s.scale * g[e];
-      const float gm = omb1 * ge;
-      m[e] = __builtin_fmaf(s.beta1, m[e], gm);
-      float gv = omb2 * ge;
-      gv = gv * ge;
-      v[e] = __builtin_fmaf(s.beta2, v[e], gv);
-      const float den = __builtin_sqrtf(v[e] * s.inv_c2) + s.eps;
-      w[e] = apply(w[e], (m[e] * s.inv_c1) / den, s);
-      amax = __builtin_elementwise_maximum(amax, __builtin_fabsf(m[e]));
-      vmax = __builtin_elementwise_maximum(vmax, v[e]);
-    }
-    amax = block_max(amax);
-    vmax = block_max(vmax);
-    const float inv_m = amax != 0.f ? 1.f / amax : 0.f, inv_v = vmax != 0.f ? 1.f / vmax : 0.f;
-    cm = uint2{encode_m4(m, inv_m), encode_m4(m + 4, inv_m)};
-    cv = uint2{encode_v4(v, inv_v), encode_v4(v + 4, inv_v)};
-    if (in_block == 0) { Ms[b] = amax; Vs[b] = vmax; }
-    if (whole) {
-      *reinterpret_cast<uint2*>(Mc + o) = cm;
-      *reinterpret_cast<uint2*>(Vc + o) = cv;
-      if (MASTER) list_store<8>(X + o, w);
-      list_store<8>(W + aw, w);
-    } else {
-      const uint32_t lm[2] = {cm.x, cm.y}, lv[2] = {cv.x, cv.y};
+  for (int e = 0; e < 3; ++e)
+    if (e < n) c |= (uint32_t)p[e] << (8 * e);
+  return c;
+}
+__device__ __forceinline__ void store_code4(uint8_t* p, int n, uint32_t c) {
+  if (n >= 4) { __builtin_nontemporal_store(c, reinterpret_cast<uint32_t*>(p)); return; }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (o + e < n) {
-          uint32_t left;
-          Mc[o + e] = (uint8_t)(lm[e >> 2] >> (8 * (e & 3)));
-          Vc[o + e] = (uint8_t)(lv[e >> 2] >> (8 * (e & 3)));
-          if (MASTER) X[o + e] = w[e];
-          W[dense ? o + e : walk_w.at(o + e, left)] = (TW)w[e];
-        }
-      }
-    }
+  for (int e = 0; e < 3; ++e)
+    if (e < n) p[e] = (uint8_t)(c >> (8 * e));
+}
+__device__ __forceinline__ void load_codes(const uint8_t* p, const LaneQ8& l, bool row, uint32_t (&c)[2]) {
+  if (row && l.n1 >= 4) {
+    const q_u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const q_u32x2*>(p + l.at0));
+    c[0] = x[0]; c[1] = x[1];
+  } else {
+    c[0] = load_code4(p + l.at0, l.n0);
+    c[1] = load_code4(p + l.at1, l.n1);
+  }
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, const LaneQ8& l, bool row, const uint32_t (&c)[2]) {
+  if (row && l.n1 >= 4) {
+    __builtin_nontemporal_store(q_u32x2{c[0], c[1]}, reinterpret_cast<q_u32x2*>(p + l.at0));
+  } else {
+    store_code4(p + l.at0, l.n0, c[0]);
+    store_code4(p + l.at1, l.n1, c[1]);
   }
 }
 
@@ -258,64 +335,77 @@ __global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const AdamWQ8Gr
     if (grp.call.stats->finite != 1.f) return;
     s.scale = grp.call.stats->scale;
   }
-  const int i = tensor_of_block(grp.begin, grp.call.count, blockIdx.x);
+  const int block = grp.call.block0 + span_of_block();
+  const int i = tensor_of_block(grp.begin, grp.call.count, block);
   const AdamWQ8Tensor& p = grp.t[i];
   s.keep = p.keep;
-  const int64_t first = (int64_t)(blockIdx.x - grp.begin[i]) * grp.call.span, rest = p.count - first;
-  const int n = rest < grp.call.span ? (int)rest : grp.call.span;
-  const bool master = p.master != nullptr;
-  switch (grp.types[i]) {
-    case 0: adamw_q8_span<float, float, false>(p, s, first, n); break;
-    case 2: adamw_q8_span<float, __bf16, false>(p, s, first, n); break;
-    case 1:
-      if (master) adamw_q8_span<__bf16, float, true>(p, s, first, n);
-      else adamw_q8_span<__bf16, float, false>(p, s, first, n);
-      break;
-    default:
-      if (master) adamw_q8_span<__bf16, __bf16, true>(p, s, first, n);
-      else adamw_q8_span<__bf16, __bf16, false>(p, s, first, n);
+  const int64_t first = (int64_t)(block - grp.begin[i]) * kSpanQ8, rest = p.count - first;
+  const int n = rest < kSpanQ8 ? (int)rest : kSpanQ8;
+  const int types = grp.types[i] + (p.master ? 4 : 0);
+  const int b = threadIdx.x / kLanes, base = b * kBlock, len = n - base;
+  if (len <= 0) return;   // the 32 lanes of a block stay together
+  // A lane's elements: 8 in a row where 16 bytes hold them (bf16), else 4 and the 4 that are 128 further on, so that the
+  // lanes' 16-byte accesses follow each other (60M fp32 elements: 178 us with 8 in a row, 157 with 4 and half the lanes).
+  const bool row = types == 3;
+  const int lane = threadIdx.x % kLanes, at0 = base + (row ? lane * 8 : lane * 4), at1 = row ? at0 + 4 : at0 + kBlock / 2;
+  const LaneQ8 l{first, at0, at1, n - at0, n - at1, p.ldw == p.cols && p.ldg == p.cols && len >= kBlock};
+  uint8_t* const Mc = p.Mc + first;
+  uint8_t* const Vc = p.Vc + first;
+  float* const Ms = p.Ms + (first >> 8);
+  float* const Vs = p.Vs + (first >> 8);
+  uint32_t cm[2], cv[2];
+  load_codes(Mc, l, row, cm);
+  load_codes(Vc, l, row, cv);
+  float sm = Ms[b], sv = Vs[b];
+  ListF32<8> g, w;
+  switch (types) {
+    case 0: load_q8<float, float, false, false>(p, l, g, w); break;
+    case 1: load_q8<__bf16, float, false, false>(p, l, g, w); break;
+    case 2: load_q8<float, __bf16, false, false>(p, l, g, w); break;
+    case 3: load_q8<__bf16, __bf16, false, true>(p, l, g, w); break;
+    case 5: load_q8<__bf16, float, true, false>(p, l, g, w); break;
+    default: load_q8<__bf16, __bf16, true, false>(p, l, g, w);
+  }
+  step_q8(g, w, cm, cv, sm, sv, s);
+  if (lane == 0) { Ms[b] = sm; Vs[b] = sv; }
+  store_codes(Mc, l, row, cm);
+  store_codes(Vc, l, row, cv);
+  switch (types) {
+    case 0: case 2: store_q8<float, false, false>(p, l, w); break;
+    case 1: store_q8<__bf16, false, false>(p, l, w); break;
+    case 3: store_q8<__bf16, false, true>(p, l, w); break;
+    default: store_q8<__bf16, true, false>(p, l, w);
   }
 }
 
-// Elements per workgroup for a list, and the first workgroup of every tensor; returns the number of workgroups, 0 if the
-// list does not fit one launch.
-template <class Group> int64_t lay_out(Group& g) {
-  int64_t total = 0;
-  for (int i = 0; i < g.call.count; ++i) total += g.t[i].count;
-  int64_t span = 2048;
-  int64_t blocks;
-  for (;; span *= 2) {
-    blocks = 0;
-    for (int i = 0; i < g.call.count; ++i) {
-      g.begin[i] = (int32_t)blocks;
-      blocks += (g.t[i].count + span - 1) / span;
-      if (blocks > kMaxBlocks) break;
-    }
-    if (blocks <= kMaxBlocks && (total <= (int64_t)1 << 22 || span >= 8192)) break;
-    if (span >= (int64_t)1 << 19) return 0;
+// Spans of the list's tensors and the launches over them: one, unless a launch cannot have so many workgroups.
+template <class Group, class Kernel> hipError_t launch_spans(Group& g, int64_t span, Kernel kernel, hipStream_t stream) {
+  int64_t blocks = 0;
+  for (int i = 0; i < g.call.count; ++i) {
+    g.begin[i] = (int32_t)blocks;
+    blocks += (g.t[i].count + span - 1) / span;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
   }
-  g.call.span = (int32_t)span;
-  return blocks;
+  for (int64_t b = 0; b < blocks; b += kMaxBlocks) {
+    g.call.block0 = (int32_t)b;
+    const int64_t grid = blocks - b < kMaxBlocks ? blocks - b : kMaxBlocks;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
 hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream) {
-  if (g.call.count <= 0) return hipSuccess;
   if (g.call.count > kAdamWTensors) return hipErrorInvalidValue;
-  const int64_t blocks = lay_out(g);
-  if (blocks == 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(adamw_list_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, g);
-  return hipGetLastError();
+  return launch_spans(g, kSpan, adamw_list_kernel, stream);
 }
 
 hipError_t launch_adamw_q8(AdamWQ8Group& g, hipStream_t stream) {
-  if (g.call.count <= 0) return hipSuccess;
   if (g.call.count > kAdamWQ8Tensors) return hipErrorInvalidValue;
-  const int64_t blocks = lay_out(g);
-  if (blocks == 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(adamw_q8_list_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, g);
-  return hipGetLastError();
+  return launch_spans(g, kSpanQ8, adamw_q8_list_kernel, stream);
 }
 
 }  // namespace galore

@@ -47,7 +47,7 @@ struct AdamWCall {
   float beta1, beta2, eps, lr;
   float inv_c1, inv_c2;    // 1 / (1 - beta^k)
   int32_t count;
-  int32_t span;            // elements per workgroup
+  int32_t block0;          // first workgroup of the launch in the list
 };
 
 template <class Tensor, int N> struct AdamWList {
@@ -60,7 +60,7 @@ typedef AdamWList<AdamWTensor, kAdamWTensors> AdamWGroup;
 typedef AdamWList<AdamWQ8Tensor, kAdamWQ8Tensors> AdamWQ8Group;
 static_assert(sizeof(AdamWGroup) <= 4096 && sizeof(AdamWQ8Group) <= 4096, "kernel arguments");
 
-// The host fills everything but begin and span.
+// The host fills everything but begin and block0.
 hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream);
 hipError_t launch_adamw_q8(AdamWQ8Group& g, hipStream_t stream);
 
