@@ -5,6 +5,9 @@ gradient of a layer has been accumulated, the hook calls `galore_step` for that 
 the tensor list and drops the gradients, so full-size gradients of at most one layer are alive at
 a time and the optimizer work of layer l overlaps with the backward pass of layer l - 1.
 
+Parameters that GaLore leaves alone (norm weights, embeddings, output head) can be given as `others`: `finish()` steps
+them with the library's AdamW, all in one call.
+
 Only marshalling lives here: every arithmetic step runs in the library.  The library's streams are
 joined into torch's current stream by `finish()`, which the training loop calls after `backward()`
 (before the next forward pass reads the weights).
@@ -15,10 +18,12 @@ from . import binding as gb
 
 
 class PerLayerGaLore:
-    def __init__(self, layers, rank, lr, overlap_calls=True, **kwargs):
+    def __init__(self, layers, rank, lr, overlap_calls=True, others=(), others_lr=None, others_options=None, **kwargs):
         """layers: list of lists of 2-D parameters (one inner list per transformer block, in the order
         the library should see them).  overlap_calls: False, True (two calls in flight) or 3 (three; pass
-        workspace_factor=3 too, so that refreshes overlap as well).  kwargs go to `binding.GaLore`
+        workspace_factor=3 too, so that refreshes overlap as well).  others: parameters of any rank for AdamW, with
+        learning rate others_lr (default: lr); others_options go to `binding.GaLoreAdamW` (moments, master,
+        weight_decay, ...).  kwargs go to `binding.GaLore`
         (update_gap, scale, moments, workspace_factor, ...)."""
         self.layers = [list(l) for l in layers]
         self.flat = [p for l in self.layers for p in l]
@@ -37,6 +42,10 @@ class PerLayerGaLore:
         self._lib_streams = self.opt.library_streams() if overlap_calls else []
         # the weights stay where they are: their argument arrays are marshalled once
         self._w_arrays = [gb.tensor_array(gb.desc(p.data) for p in l) for l in self.layers]
+        self.others = list(others)
+        self.others_lr = lr if others_lr is None else others_lr
+        self.others_opt = gb.GaLoreAdamW([p.data for p in self.others], **(others_options or {})) if self.others else None
+        self._others_array = gb.tensor_array(gb.param_desc(p.data) for p in self.others)
         self._ready = [0] * len(self.layers)
         self._handles = []
         for li, l in enumerate(self.layers):
@@ -63,8 +72,17 @@ class PerLayerGaLore:
         for p in params:
             p.grad = None
 
-    def finish(self):
-        """Call after backward(): orders the library's streams before torch's current stream."""
+    def finish(self, stats=None):
+        """Call after backward(): steps the other parameters and drops their gradients, and orders the library's
+        streams before torch's current stream.  stats: what a `binding.GaLoreGradNorm` measured of the other
+        parameters' gradients (those of the GaLore matrices are gone by now)."""
+        if self.others:
+            grads = [p.grad for p in self.others]
+            if any(g is None for g in grads):
+                raise ValueError("a parameter of `others` has no gradient")
+            self.others_opt.step(self._others_array, grads, self.others_lr, stats)
+            for p in self.others:
+                p.grad = None
         self.opt.join()
 
     def close(self):

@@ -6,7 +6,7 @@ A stack of decoder blocks (RMSNorm, causal self-attention without biases, SwiGLU
 weights, random hidden states as input; embedding and LM head left out) runs forward + backward
   (a) alone, gradients dropped;
   (b) with `hooks.PerLayerGaLore`: each block's 7 matrices are stepped by the library as soon as
-      their gradients exist;
+      their gradients exist, and all norm weights by the library's AdamW after the backward pass;
   (c) with torch's fused AdamW on the same matrices after the backward pass, for scale.
 Prints ONE JSON line with tokens/s of each and the overhead of (b) over (a).
 
@@ -42,6 +42,9 @@ class DecoderBlock(torch.nn.Module):
         self.n1, self.n2 = RMSNorm(d, dtype), RMSNorm(d, dtype)
         self.q, self.k, self.v, self.o = lin(d, d), lin(d, d), lin(d, d), lin(d, d)
         self.gate, self.up, self.down = lin(d, f), lin(d, f), lin(f, d)
+
+    def norms(self):
+        return [self.n1.weight, self.n2.weight]
 
     def matrices(self):
         return [m.weight for m in (self.q, self.k, self.v, self.o, self.gate, self.up, self.down)]
@@ -119,7 +122,8 @@ def main(argv=None):
 
     # calls in flight, and a workspace share for each so that the refreshes of the first step overlap too
     drv = PerLayerGaLore([blk.matrices() for blk in blocks], args.rank, 1e-4, overlap_calls=args.in_flight, update_gap=200,
-                         refresh_iters=4, moments=args.moments, workspace_factor=args.in_flight)
+                         refresh_iters=4, moments=args.moments, workspace_factor=args.in_flight,
+                         others=[p for blk in blocks for p in blk.norms()], others_options={"moments": args.moments})
     drv.opt.set_fused_adam(bool(args.fused_adam))
     # the first step refreshes every projector; time it apart
     torch.cuda.synchronize()
@@ -132,8 +136,6 @@ def main(argv=None):
     def with_galore():
         fwd_bwd()
         drv.finish()
-        for p in blocks.parameters():
-            p.grad = None   # the norm weights (not GaLore matrices)
 
     ms_galore = timed(with_galore, args.reps)
     drv.close()

@@ -378,3 +378,57 @@ def test_training_descends_as_torch_does_it():
         w64, m, v, _ = ao.adamw(w64, w64 - target, m, v, B1, B2, EPS, LR, WD, k)
     # an error of a weight enters the next gradients; 20 steps of at most 30 roundings of numbers under 8 each
     assert np.abs(to64(W) - w64).max() <= 20 * 30 * 8 * U
+
+
+@pytest.mark.parametrize("moments", ["f32", "q8"])
+def test_hooks_step_the_other_parameters(moments):
+    # a training loop with GaLore matrices and norm weights through PerLayerGaLore, against the same steps by hand
+    from paper_2403_03507_amd.hooks import PerLayerGaLore
+
+    class Block(torch.nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.scale = torch.nn.Parameter(torch.ones(64, device="cuda"))
+            self.up = torch.nn.Linear(64, 192, bias=False, device="cuda")
+            self.down = torch.nn.Linear(192, 64, bias=True, device="cuda")
+
+        def forward(self, x):
+            return x + self.down(torch.nn.functional.silu(self.up(x * self.scale)))
+
+    def model():
+        torch.manual_seed(5)
+        return torch.nn.Sequential(Block(), Block())
+
+    xs = [torch.randn(32, 64, device="cuda", generator=torch.Generator("cuda").manual_seed(50 + s)) for s in range(3)]
+    mats = lambda net: [[b.up.weight, b.down.weight] for b in net]
+    rest = lambda net: [p for b in net for p in (b.scale, b.down.bias)]
+    hooked = model()
+    drv = PerLayerGaLore(mats(hooked), 8, 1e-2, update_gap=2, refresh_iters=3, others=rest(hooked), others_lr=3e-2,
+                         others_options={"moments": moments, "weight_decay": [0.0, 0.1, 0.0, 0.1]})
+    norm = gb.GaLoreGradNorm(4, max_norm=0.01)
+    for i, x in enumerate(xs):
+        hooked(x).pow(2).mean().backward()
+        drv.finish(norm.measure([p.grad for p in rest(hooked)]) if i else None)
+        assert all(p.grad is None for p in hooked.parameters())
+    manual = model()
+    flat, others = [p for l in mats(manual) for p in l], rest(manual)
+    opt = gb.GaLore([p.data for p in flat], 8, update_gap=2, refresh_iters=3)
+    adamw = gb.GaLoreAdamW(others, moments=moments, weight_decay=[0.0, 0.1, 0.0, 0.1])
+    for i, x in enumerate(xs):
+        manual(x).pow(2).mean().backward()
+        for li in (1, 0):
+            ps = flat[2 * li:2 * li + 2]
+            opt.step([p.data for p in ps], [p.grad for p in ps], 1e-2, first=2 * li)
+        adamw.step([p.data for p in others], [p.grad for p in others], 3e-2, norm.measure([p.grad for p in others]) if i else None)
+        for p in manual.parameters():
+            p.grad = None
+    torch.cuda.synchronize()
+    for a, b in zip(hooked.parameters(), manual.parameters()):
+        assert torch.equal(a, b)
+    hooked(xs[0]).pow(2).mean().backward()
+    rest(hooked)[0].grad = None
+    with pytest.raises(ValueError):
+        drv.finish()
+    drv.opt.join()
+    drv.close()
+    opt.close()
