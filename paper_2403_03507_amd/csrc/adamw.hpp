@@ -72,7 +72,8 @@ struct GradTensor {
 
 struct GradGroup {
   int32_t count;
-  int32_t span;
+  int32_t span;            // norm: 1024s of elements per workgroup
+  int32_t block0;          // scaling: first workgroup of the launch in the list
   int32_t begin[kGradTensors];
   uint8_t bf16[kGradTensors];
   GradTensor t[kGradTensors];

@@ -25,29 +25,31 @@ template <int N> __device__ __forceinline__ int tensor_of_block(const int32_t (&
 }
 
 // Workgroups reach the 8 XCDs in turn: with this numbering each XCD takes runs of 512 consecutive spans, so that the
-// streams of one XCD stay in few DRAM pages (AdamW over 101M elements: 458 us numbered as launched, 452 in runs; 128
-// threads each).  Launches, and their ends, of fewer than 4096 workgroups keep their numbers.
+// streams of one XCD stay in few DRAM pages (AdamW, 128 threads each, 262M bf16 weights: 934 us numbered as launched, 912
+// in runs; 30M fp32: 135 and 132).  Launches, and their ends, of fewer than 4096 workgroups keep their numbers.
 __device__ __forceinline__ int span_of_block() {
   constexpr int kRun = 512, kXcds = 8;
   const int block = blockIdx.x, in_group = block % (kRun * kXcds), group = block - in_group;
   return group + kRun * kXcds <= (int)gridDim.x ? group + in_group % kXcds * kRun + in_group / kXcds : block;
 }
 
-// Element o of a span that starts at (row, col) of a matrix with `cols` columns, as an offset from the matrix' first
-// element.  o < 2^20 and cols < 2^30: the division is one of 32 bits.
+// Where element o of a span lies in a matrix whose rows may be apart: row and column, from which every tensor of that shape
+// finds its own offset.  o < 2^20 and cols < 2^30: the division is one of 32 bits.
 struct RowWalk {
-  int64_t row;
-  uint32_t col, cols;
-  int64_t ld;
-  __device__ __forceinline__ RowWalk(int64_t first, int32_t cols_, int32_t ld_) : cols(cols_), ld(ld_) {
-    row = first / cols_;
-    col = (uint32_t)(first - row * cols_);
+  int64_t row0;
+  uint32_t col0, cols;
+  __device__ __forceinline__ RowWalk(int64_t first, int32_t cols_) : cols(cols_) {
+    row0 = first / cols_;
+    col0 = (uint32_t)(first - row0 * cols_);
   }
-  // offset of element o, and how many elements follow it in its row (itself included)
-  __device__ __forceinline__ int64_t at(int o, uint32_t& left) const {
-    const uint32_t c = col + (uint32_t)o, r = c / cols, x = c - r * cols;
-    left = cols - x;
-    return (row + r) * ld + x;
+  struct Place {
+    int64_t row;
+    uint32_t col, left;   // left: elements of the row from this one on
+    __device__ __forceinline__ int64_t offset(int32_t ld) const { return row * ld + col; }
+  };
+  __device__ __forceinline__ Place at(int o) const {
+    const uint32_t c = col0 + (uint32_t)o, r = c / cols, x = c - r * cols;
+    return Place{row0 + r, x, cols - x};
   }
 };
 
