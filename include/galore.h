@@ -427,8 +427,8 @@ typedef struct {
  * for the next step).  Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their
  * block) non-finite.
  * One launch for up to 56 tensors with fp32 moments, or up to 44 with 8-bit ones.
- * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address; written
- * tensors that overlap otherwise are not detected and must not be passed. */
+ * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address, or a gradient
+ * does at that of one of them; tensors that overlap otherwise are not detected and must not be passed. */
 galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count,
                            float beta1, float beta2, float eps, float lr, int64_t k, const galore_grad_stats* stats,
                            void* hip_stream);

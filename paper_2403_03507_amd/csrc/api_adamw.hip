@@ -25,20 +25,26 @@ class Addresses {
     slots_.assign(n, nullptr);
   }
   bool add(const void* p) {   // false: already there
+    const void*& slot = find(p);
+    if (slot) return false;
+    slot = p;
+    return true;
+  }
+  bool has(const void* p) { return find(p) != nullptr; }
+
+ private:
+  const void*& find(const void* p) {   // p's slot, or the free one where it belongs
     size_t h = (size_t)((reinterpret_cast<uintptr_t>(p) >> 2) * 0x9E3779B97F4A7C15ull >> 20);
     for (;; ++h) {
       const void*& slot = slots_[h & (slots_.size() - 1)];
-      if (slot == p) return false;
-      if (!slot) { slot = p; return true; }
+      if (!slot || slot == p) return slot;
     }
   }
-
- private:
   std::vector<const void*> slots_;   // no tensor starts at NULL
 };
 
 galore_status fail_twice(const char* what, int i) {
-  return fail(nullptr, GALORE_ERR_INVALID_ARG, "%s[%d] starts at the same address as another tensor that the call writes", what, i);
+  return fail(nullptr, GALORE_ERR_INVALID_ARG, "%s[%d] starts at the same address as a tensor that the call writes", what, i);
 }
 
 galore_status check_stats(const galore_grad_stats* stats) {
@@ -133,6 +139,8 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
     if (!written.add(st.m.data)) return fail_twice("m", i);
     if (!written.add(st.v.data)) return fail_twice("v", i);
   }
+  for (int32_t i = 0; i < count; ++i)
+    if (written.has(G[i].data)) return fail_twice("G", i);
 
   AdamWCall call{};
   call.stats = reinterpret_cast<const GradStats*>(stats);

@@ -13,6 +13,11 @@ constexpr int kNormThreads = 512;
 // that there is no second round (33M bf16 elements: 43.6 us with 2048, 37.7 with 960; 151M: 49.9 and 50.5).
 constexpr int kPartialTarget = 2048, kOneRound = 960;
 constexpr int64_t kOneRoundElements = (int64_t)1 << 26;
+// What follows a norm (AdamW, the scaling) reads the same gradients again and finds a part of them in the 256 MiB cache if
+// they were loaded through it, which the norm itself pays for: norm and AdamW of 25 MB of gradients 53.4 us (loads past the
+// caches 56.1), 240 MB 433 (457), 400 MB 734 (772), 800 MB 1505 (1532), 1600 MB 3046 (3054); the norm alone 76 (67) at 400 MB,
+// 138 (122) at 800.
+constexpr int64_t kCachedBytes = (int64_t)512 << 20;
 constexpr int kScaleThreads = 128;
 constexpr int kScaleBytes = 2 * 16 * kScaleThreads;   // of a tensor, per workgroup: two 16-byte accesses of every thread
 
@@ -28,7 +33,7 @@ __device__ __forceinline__ double workgroup_sum(double x) {
   return all;
 }
 
-template <class T> __device__ __forceinline__ double squares(const GradTensor& p, int64_t first, int64_t n) {
+template <class T, bool CACHED> __device__ __forceinline__ double squares(const GradTensor& p, int64_t first, int64_t n) {
   constexpr int N = 16 / sizeof(T);
   constexpr int kPiece = 1 << 19;   // offsets that RowWalk takes
   const T* G = static_cast<const T*>(p.G);
@@ -43,12 +48,12 @@ template <class T> __device__ __forceinline__ double squares(const GradTensor& p
     G += first;
     int64_t o = (int64_t)threadIdx.x * N;
     for (; o + kStep + N <= n; o += 2 * kStep) {   // two requests at a time
-      const ListF32<N> a = list_load<N>(G + o), b = list_load<N>(G + o + kStep);
+      const ListF32<N> a = list_load<N, CACHED>(G + o), b = list_load<N, CACHED>(G + o + kStep);
       add(a);
       add(b);
     }
     for (; o < n; o += kStep) {
-      if (o + N <= n) add(list_load<N>(G + o));
+      if (o + N <= n) add(list_load<N, CACHED>(G + o));
       else for (int64_t e = o; e < n; ++e) one(G[e]);
     }
   } else {
@@ -57,7 +62,7 @@ template <class T> __device__ __forceinline__ double squares(const GradTensor& p
       const int len = n - base < kPiece ? (int)(n - base) : kPiece;
       for (int o = threadIdx.x * N; o < len; o += kNormThreads * N) {
         const RowWalk::Place at = walk.at(o);
-        if (o + N <= len && at.left >= N) add(list_load<N>(G + at.offset(p.ld)));
+        if (o + N <= len && at.left >= N) add(list_load<N, CACHED>(G + at.offset(p.ld)));
         else for (int e = o; e < o + N && e < len; ++e) one(G[walk.at(e).offset(p.ld)]);
       }
     }
@@ -68,12 +73,12 @@ template <class T> __device__ __forceinline__ double squares(const GradTensor& p
   return all;
 }
 
-__global__ __launch_bounds__(kNormThreads) void grad_squares_kernel(const GradGroup grp, double* partials) {
+template <bool CACHED> __global__ __launch_bounds__(kNormThreads) void grad_squares_kernel(const GradGroup grp, double* partials) {
   const int i = tensor_of_block(grp.begin, grp.count, blockIdx.x);
   const GradTensor& p = grp.t[i];
   const int64_t span = (int64_t)grp.span * 1024, first = (blockIdx.x - grp.begin[i]) * span, rest = p.count - first;
   const int64_t n = rest < span ? rest : span;
-  const double x = workgroup_sum(grp.bf16[i] ? squares<__bf16>(p, first, n) : squares<float>(p, first, n));
+  const double x = workgroup_sum(grp.bf16[i] ? squares<__bf16, CACHED>(p, first, n) : squares<float, CACHED>(p, first, n));
   if (threadIdx.x == 0) partials[blockIdx.x] = x;
 }
 
@@ -154,9 +159,13 @@ template <class F> int64_t lay_out(GradGroup& g, F elements) {
 size_t grad_norm_partials(int32_t count) { return (size_t)kPartialTarget + (size_t)count; }
 
 hipError_t launch_grad_norm(GradGroup* lists, int n_lists, float grad_scale, float max_norm, GradStats* stats, double* partials, hipStream_t stream) {
-  int64_t total = 0;
+  int64_t total = 0, bytes = 0;
   for (int l = 0; l < n_lists; ++l)
-    for (int i = 0; i < lists[l].count; ++i) total += lists[l].t[i].count;
+    for (int i = 0; i < lists[l].count; ++i) {
+      total += lists[l].t[i].count;
+      bytes += lists[l].t[i].count * (lists[l].bf16[i] ? 2 : 4);
+    }
+  const auto kernel = bytes <= kCachedBytes ? grad_squares_kernel<true> : grad_squares_kernel<false>;
   // sum over tensors of ceil(count / elements) <= total / elements + tensors <= kPartialTarget + tensors
   const int64_t target = (int64_t)(total <= kOneRoundElements ? kOneRound : kPartialTarget) * 1024;
   int64_t span = (total + target - 1) / target;
@@ -167,7 +176,7 @@ hipError_t launch_grad_norm(GradGroup* lists, int n_lists, float grad_scale, flo
     const int64_t blocks = lay_out(lists[l], [&](int) { return span * 1024; });
     if (blocks < 0) return hipErrorInvalidValue;
     lists[l].span = (int32_t)span;
-    hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, lists[l], partials + done);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, lists[l], partials + done);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     done += blocks;

@@ -66,9 +66,11 @@ template <> struct ListVec<float, 8> { typedef list_f32x8_any type; };
 template <> struct ListVec<__bf16, 8> { typedef list_bf16x8_any type; };
 template <int N> using ListF32 = float __attribute__((ext_vector_type(N)));
 
-template <int N, class T> __device__ __forceinline__ ListF32<N> list_load(const T* p) {
+// CACHED: another kernel is about to read the same again; else past the caches
+template <int N, bool CACHED = false, class T> __device__ __forceinline__ ListF32<N> list_load(const T* p) {
   typedef typename ListVec<T, N>::type V;
-  return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const V*>(p)), ListF32<N>);
+  const V* v = reinterpret_cast<const V*>(p);
+  return __builtin_convertvector(CACHED ? *v : __builtin_nontemporal_load(v), ListF32<N>);
 }
 template <int N, class T> __device__ __forceinline__ void list_store(T* p, ListF32<N> x) {
   typedef typename ListVec<T, N>::type V;

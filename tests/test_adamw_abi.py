@@ -121,6 +121,13 @@ def test_adamw_refuses_the_same_tensor_twice():
     assert c.status() == 1
 
 
+def test_adamw_refuses_a_gradient_that_it_would_overwrite():
+    c = Call(); c.G[0].data = c.W[1].data
+    assert c.status() == 1
+    c = Call(); c.G[1].data = c.S[0].m.data
+    assert c.status() == 1
+
+
 def test_gradient_calls_refuse_bad_arguments():
     L = gb.lib()
     need = gb.galore_grad_norm_workspace_bytes(2)

@@ -162,6 +162,28 @@ def test_eight_bit_moments_equal_the_format_bit_for_bit(master):
             assert _outside_is_nan(*W[i])
 
 
+@pytest.mark.parametrize("size", [1e-38, 1e-25, 1e-20, 1e-10, 1e6, 1e12, 1e18])
+def test_eight_bit_moments_at_extreme_magnitudes(size):
+    # scales that are subnormal or zero (reciprocals beyond fp32), and second moments beyond 2^31 times their codes' range
+    rng = np.random.default_rng(6)
+    w = torch.from_numpy(rng.standard_normal((3, 700))).float().cuda()
+    opt = gb.GaLoreAdamW([w], moments="q8", beta1=B1, beta2=B2, eps=EPS)
+    n = w.numel()
+    Mc, Vc, Ms, Vs = np.zeros(n, np.uint8), np.zeros(n, np.uint8), np.zeros(9, np.float32), np.zeros(9, np.float32)
+    for k in range(1, 4):
+        g = (rng.standard_normal(n) * size).astype(np.float32)
+        before = to64(w).reshape(-1)
+        opt.step([w], [torch.from_numpy(g).view(3, 700).cuda()], LR)
+        want_n = q8.adam_q8(g, Mc, Vc, Ms, Vs, B1, B2, EPS, k).astype(np.float64)
+        got = opt.M[0].cpu().numpy().reshape(-1)
+        assert np.array_equal(np.where(got == 0x80, 0, got), np.where(Mc == 0x80, 0, Mc)), k
+        assert np.array_equal(opt.V[0].cpu().numpy().reshape(-1), Vc), k
+        assert np.array_equal(opt.M_scale[0].cpu().numpy(), Ms) and np.array_equal(opt.V_scale[0].cpu().numpy(), Vs), k
+        want = before - LR * want_n
+        # as in the test above; a square root below 1.1e-19 counts as that, 1.1e-11 of the smallest denominator eps
+        _within(to64(w).reshape(-1), want, 2 * U * np.abs(before) + LR * 12 * U * np.abs(want_n) + U * np.abs(want))
+
+
 def test_blocks_of_256_are_those_of_the_low_rank_state():
     # a matrix with rows of a multiple of 256 elements: the same codes and scales as galore_adam_q8 leaves
     rng = np.random.default_rng(3)
@@ -364,6 +386,30 @@ def test_calls_run_on_the_current_stream():
     side.synchronize()
     # first step: n = 1 up to rounding (m c1 = g, sqrt(v c2) = g)
     assert float((w + 1e-2).abs().max()) <= 1e-2 * 16 * U
+
+
+def test_two_calls_at_once_on_two_streams():
+    # no state is shared between calls: two lists, two norms, two streams, no ordering between them
+    torch.manual_seed(2)
+    lists = [[torch.randn(300, 1000, device="cuda"), torch.randn(77, device="cuda")] for _ in range(2)]
+    grads = [[torch.randn_like(w) for w in ws] for ws in lists]
+    start = [[w.clone() for w in ws] for ws in lists]
+    opts = [gb.GaLoreAdamW(ws, moments=m, weight_decay=0.1) for ws, m in zip(lists, ("f32", "q8"))]
+    norms = [gb.GaLoreGradNorm(2, max_norm=1.0) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                opts[i].step(lists[i], grads[i], 1e-2, norms[i].measure(grads[i]))
+    torch.cuda.synchronize()
+    for i, m in enumerate(("f32", "q8")):
+        ref, norm = gb.GaLoreAdamW(start[i], moments=m, weight_decay=0.1), gb.GaLoreGradNorm(2, max_norm=1.0)
+        for _ in range(5):
+            ref.step(start[i], grads[i], 1e-2, norm.measure(grads[i]))
+        for a, b in zip(start[i], lists[i]):
+            assert torch.equal(a, b)
+        assert torch.equal(ref.M_flat, opts[i].M_flat) and torch.equal(ref.V_flat, opts[i].V_flat)
 
 
 def test_training_descends_as_torch_does_it():

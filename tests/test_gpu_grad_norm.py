@@ -55,6 +55,28 @@ def test_norm_of_lists(scale, max_norm):
     assert torch.equal(first, norm.measure(G, scale))                       # the order of the sum is fixed
 
 
+def test_norm_of_more_than_the_cache_holds():
+    # 600 MiB of bf16 gradients: loads past the caches, and spans of 154 thousand elements
+    rng = np.random.default_rng(1)
+    one = torch.from_numpy(rng.standard_normal(1 << 20)).bfloat16().cuda()
+    G = [one.repeat(150), one.repeat(150)[1:]]
+    total = 300 * float(one.double().square().sum()) - float(one[0]) ** 2
+    stats = gb.GaLoreGradNorm(2, max_norm=1.0).measure(G)
+    assert abs(float(stats[0]) - total ** 0.5) <= HALF * total ** 0.5
+
+
+def test_more_gradients_than_the_workspace_is_for():
+    norm = gb.GaLoreGradNorm(2)
+    G = [torch.ones(4, device="cuda") for _ in range(200)]
+    with pytest.raises(gb.GaloreError) as e:
+        norm.measure(G)
+    assert e.value.status == 6
+    norm.stats.copy_(torch.tensor([1.0, 0.5, 1.0, 0.0]))
+    with pytest.raises(gb.GaloreError) as e:
+        norm.scale([G[0], G[0]])                                                # the same tensor twice
+    assert e.value.status == 1 and bool((G[0] == 1).all())
+
+
 def test_norm_of_nothing():
     norm = gb.GaLoreGradNorm(0, max_norm=2.0)
     assert norm.measure([]).tolist() == [0.0, 1.0, 1.0, 0.0]
