@@ -387,7 +387,7 @@ galore_status galore_adafactor(const galore_tensor* R, const galore_tensor* M, c
  * What a training program needs beside galore_step: the step of the parameters GaLore leaves alone (embeddings, output
  * head, norm weights; or a whole stack at full rank, the baseline the paper compares with), and gradient clipping over
  * all of them.  No context; nothing is allocated, and everything may be captured into a HIP graph (a replay repeats the
- * call with the same lr and k).  All tensors are BORROWED device memory; a vector is a matrix of one row.  Lists of any
+ * call with the lr and k it was captured with, unless they come from a galore_adamw_clock).  All tensors are BORROWED device memory; a vector is a matrix of one row.  Lists of any
  * length; count == 0 is valid.  Errors as for the other context-free calls (galore_last_error(NULL)).
  *
  * What galore_grad_norm writes, in DEVICE memory, 16-byte aligned: the calls after it on the stream read it there, no
@@ -418,20 +418,37 @@ typedef struct {
   float weight_decay;
 } galore_adamw_state;
 
+/* Step count and learning rate in DEVICE memory, 8-byte aligned: for steps that are captured into a graph and replayed, and
+ * for counts that leave out the steps whose gradients were not finite.  The caller writes t and lr (t = 0 before the first
+ * step; lr whenever it changes, ordered by the stream); galore_adamw_tick fills in the rest. */
+typedef struct {
+  int64_t t;        /* steps begun */
+  float lr;
+  float inv_c1;     /* 1 / (1 - beta1^t), 1 / (1 - beta2^t) */
+  float inv_c2;
+  float reserved;
+} galore_adamw_clock;
+
+/* Begin a step: t <- t + 1 and its bias corrections.  Nothing changes if stats is given and stats->finite is not 1.  One
+ * tick serves every galore_adamw call of the step that has these betas. */
+galore_status galore_adamw_tick(galore_adamw_clock* clock, float beta1, float beta2, const galore_grad_stats* stats,
+                                void* hip_stream);
+
 /* One AdamW step of tensors W[0..count-1] with gradients G[i] of W[i]'s shape (fp32 or bf16, independent of W's type; any
  * ld, any element alignment).  k >= 1 is the 1-based step of the bias correction.  With g = stats->scale * G (stats NULL:
  * g = G):
  *     m <- beta1 m + (1-beta1) g ;  v <- beta2 v + (1-beta2) g^2
  *     W <- (1 - lr*weight_decay) W - lr (m / (1-beta1^k)) / (sqrt(v / (1-beta2^k)) + eps)
- * in fp32, W rounded once.  If stats->finite is not 1 the call leaves every tensor as it was (k is the caller's: repeat it
- * for the next step).  Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their
+ * in fp32, W rounded once.  With a clock (else NULL), lr and k are those on the device and the arguments are not used.
+ * If stats->finite is not 1 the call leaves every tensor as it was (a k of the caller's should then be used once more).
+ * Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their
  * block) non-finite.
  * One launch for up to 56 tensors with fp32 moments, or up to 44 with 8-bit ones.
  * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address, or a gradient
  * does at that of one of them; tensors that overlap otherwise are not detected and must not be passed. */
 galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count,
-                           float beta1, float beta2, float eps, float lr, int64_t k, const galore_grad_stats* stats,
-                           void* hip_stream);
+                           float beta1, float beta2, float eps, float lr, int64_t k, const galore_adamw_clock* clock,
+                           const galore_grad_stats* stats, void* hip_stream);
 
 /* Bytes of device workspace (256-byte aligned) galore_grad_norm needs for a list of `count` gradients. */
 galore_status galore_grad_norm_workspace_bytes(int32_t count, size_t* out_bytes);

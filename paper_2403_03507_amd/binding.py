@@ -41,6 +41,11 @@ class galore_grad_stats(ctypes.Structure):
     _fields_ = [("norm", ctypes.c_float), ("scale", ctypes.c_float), ("finite", ctypes.c_float), ("reserved", ctypes.c_float)]
 
 
+class galore_adamw_clock(ctypes.Structure):
+    _fields_ = [("t", ctypes.c_int64), ("lr", ctypes.c_float), ("inv_c1", ctypes.c_float), ("inv_c2", ctypes.c_float),
+                ("reserved", ctypes.c_float)]
+
+
 class galore_adamw_state(ctypes.Structure):
     _fields_ = [("m", galore_tensor), ("v", galore_tensor), ("m_scale", galore_tensor), ("v_scale", galore_tensor),
                 ("master", galore_tensor), ("weight_decay", ctypes.c_float)]
@@ -66,7 +71,7 @@ EXPORTS = ["galore_status_string", "galore_workspace_bytes", "galore_init", "gal
            "galore_set_call_overlap", "galore_set_fused_adam", "galore_join", "galore_get_stream",
            "galore_two_sided_workspace_bytes", "galore_two_sided_step", "galore_two_sided_refresh",
            "galore_adafactor_workspace_bytes", "galore_adafactor_step", "galore_adafactor_refresh", "galore_adafactor",
-           "galore_adamw", "galore_grad_norm_workspace_bytes", "galore_grad_norm", "galore_scale_grads"]
+           "galore_adamw", "galore_adamw_tick", "galore_grad_norm_workspace_bytes", "galore_grad_norm", "galore_scale_grads"]
 STAGES = ["project_left", "project_right", "adam", "back", "transpose", "refresh"]
 
 _lib = None
@@ -114,7 +119,8 @@ def lib():
         L.galore_adafactor_refresh.argtypes = [hp, tp, afp, vp, ctypes.c_size_t, vp]
         L.galore_adafactor.argtypes = [tp, tp, tp, tp, tp, f32, i64, vp, ctypes.c_size_t, vp]
         asp = ctypes.POINTER(galore_adamw_state)
-        L.galore_adamw.argtypes = [tp, tp, asp, i32, f32, f32, f32, f32, i64, vp, vp]
+        L.galore_adamw.argtypes = [tp, tp, asp, i32, f32, f32, f32, f32, i64, vp, vp, vp]
+        L.galore_adamw_tick.argtypes = [vp, f32, f32, vp, vp]
         L.galore_grad_norm_workspace_bytes.argtypes = [i32, ctypes.POINTER(ctypes.c_size_t)]
         L.galore_grad_norm.argtypes = [tp, i32, f32, f32, vp, vp, ctypes.c_size_t, vp]
         L.galore_scale_grads.argtypes = [tp, i32, vp, vp]
@@ -394,12 +400,26 @@ def _stats_ptr(stats):
     return stats.data_ptr()
 
 
-def galore_adamw(W, G, states, beta1, beta2, eps, lr, k, stats=None):
-    """W, G: lists of tensors or arrays of descriptors; states: list or array of galore_adamw_state."""
+def _clock_ptr(clock):
+    if clock is None:
+        return None
+    if not clock.is_cuda or clock.get_device() != torch._C._cuda_getDevice() or clock.dtype != torch.uint8 \
+            or clock.shape != (ctypes.sizeof(galore_adamw_clock),) or clock.stride(0) != 1:
+        raise ValueError("clock: %d contiguous bytes on the current device" % ctypes.sizeof(galore_adamw_clock))
+    return clock.data_ptr()
+
+
+def galore_adamw(W, G, states, beta1, beta2, eps, lr, k, stats=None, clock=None):
+    """W, G: lists of tensors or arrays of descriptors; states: list or array of galore_adamw_state; clock: 24 bytes on the
+    device (galore_adamw_clock) that lr and k are then taken from."""
     W, G, S = _param_array(W), _param_array(G), _arr(states, galore_adamw_state)
     if not len(W) == len(G) == len(S):
         raise ValueError("weights, gradients and states differ in number")
-    _check(lib().galore_adamw(W, G, S, len(W), beta1, beta2, eps, lr, int(k), _stats_ptr(stats), _stream()))
+    _check(lib().galore_adamw(W, G, S, len(W), beta1, beta2, eps, lr, int(k), _clock_ptr(clock), _stats_ptr(stats), _stream()))
+
+
+def galore_adamw_tick(clock, beta1, beta2, stats=None):
+    _check(lib().galore_adamw_tick(_clock_ptr(clock), beta1, beta2, _stats_ptr(stats), _stream()))
 
 
 def galore_grad_norm_workspace_bytes(count):
@@ -446,11 +466,15 @@ class GaLoreGradNorm:
 class GaLoreAdamW:
     """AdamW for a list of parameters that GaLore leaves alone (any rank; embeddings, norm weights, biases): owns their
     moments and, with master=True, fp32 master copies of the bf16 ones (torch memory, one flat buffer per kind), and
-    keeps the step count; all arithmetic happens in the library."""
+    keeps the step count; all arithmetic happens in the library.
+
+    With capturable=True the count and the learning rate live on the device (`clock`): a step that is captured into a graph
+    counts on every replay with the rate that set_lr() left there, and steps whose gradients were not finite do not count."""
 
     _ALIGN = 256  # elements: the states of every tensor start at a multiple (16-byte alignment, blocks of the 8-bit format)
 
-    def __init__(self, weights, moments="f32", master=False, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, device="cuda"):
+    def __init__(self, weights, moments="f32", master=False, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, device="cuda",
+                 capturable=False):
         """moments: "f32" or "q8" (8-bit codes, one fp32 scale per 256 elements).  weight_decay: a number, or one per tensor."""
         if moments not in ("f32", "q8"):
             raise ValueError("moments: f32 or q8")
@@ -486,11 +510,27 @@ class GaLoreAdamW:
                                              param_desc(self.V_scale[i]) if q8 else none,
                                              like(self.master[i]) if self.master[i] is not None else none, decay[i]))
         self._states = (galore_adamw_state * len(states))(*states)
+        self.clock = torch.zeros(ctypes.sizeof(galore_adamw_clock), dtype=torch.uint8, device=device) if capturable else None
 
-    def step(self, weights, grads, lr, stats=None):
-        """weights, grads: tensors in the constructor's order, or arrays of their descriptors.  stats: the result of a
-        GaLoreGradNorm; its factor is applied to the gradients, and where an entry was not finite nothing changes (the
-        step is counted all the same: set `t` back to repeat it)."""
+    def set_lr(self, lr):
+        """capturable: the learning rate of the steps from here on (ordered by the current stream)."""
+        self.clock[8:12].view(torch.float32).fill_(lr)
+
+    def count(self):
+        """Steps taken; capturable: read from the device, which waits for it."""
+        return self.t if self.clock is None else int(self.clock[:8].view(torch.int64))
+
+    def step(self, weights, grads, lr=None, stats=None):
+        """weights, grads: tensors in the constructor's order, or arrays of their descriptors.  lr: with capturable=True
+        None, or set_lr() first.  stats: the result of a GaLoreGradNorm; its factor is applied to the gradients, and where
+        an entry was not finite nothing changes (without capturable the step is counted all the same: set `t` back to
+        repeat it)."""
+        if self.clock is not None:
+            if lr is not None:
+                self.set_lr(lr)
+            galore_adamw_tick(self.clock, self.beta1, self.beta2, stats)
+            galore_adamw(weights, grads, self._states, self.beta1, self.beta2, self.eps, 0.0, 1, stats, self.clock)
+            return
         galore_adamw(weights, grads, self._states, self.beta1, self.beta2, self.eps, lr, self.t + 1, stats)
         self.t += 1
 

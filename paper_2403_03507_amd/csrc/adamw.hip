@@ -24,6 +24,15 @@ struct Scalars {
   float scale, beta1, beta2, eps, lr, inv_c1, inv_c2, keep;
 };
 
+// What the tensors of a call have in common; false: the step is left out.
+__device__ __forceinline__ bool scalars(const AdamWCall& c, Scalars& s) {
+  s = Scalars{1.f, c.beta1, c.beta2, c.eps, c.lr, c.inv_c1, c.inv_c2, 1.f};
+  if (c.clock) { s.lr = c.clock->lr; s.inv_c1 = c.clock->inv_c1; s.inv_c2 = c.clock->inv_c2; }
+  if (!c.stats) return true;
+  s.scale = c.stats->scale;
+  return c.stats->finite == 1.f;
+}
+
 __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { return __builtin_fmaf(-s.lr, n, s.keep * w); }
 
 // ---- fp32 moments ----------------------------------------------------------------------------------
@@ -80,15 +89,12 @@ __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& 
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup grp) {
-  Scalars s{1.f, grp.call.beta1, grp.call.beta2, grp.call.eps, grp.call.lr, grp.call.inv_c1, grp.call.inv_c2, 1.f};
-  if (grp.call.stats) {
-    if (grp.call.stats->finite != 1.f) return;  // the whole step is left out
-    s.scale = grp.call.stats->scale;
-  }
+  Scalars s;
+  if (!scalars(grp.call, s)) return;
   const int block = grp.call.block0 + span_of_block();
   const int i = tensor_of_block(grp.begin, grp.call.count, block);
   const AdamWTensor& p = grp.t[i];
-  s.keep = p.keep;
+  s.keep = __builtin_fmaf(-s.lr, p.decay, 1.f);
   const int64_t first = (int64_t)(block - grp.begin[i]) * kSpan, rest = p.count - first;
   const int n = rest < kSpan ? (int)rest : kSpan;
   const bool master = p.master != nullptr;
@@ -352,15 +358,12 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const LaneQ8& l, bool ro
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const AdamWQ8Group grp) {
-  Scalars s{1.f, grp.call.beta1, grp.call.beta2, grp.call.eps, grp.call.lr, grp.call.inv_c1, grp.call.inv_c2, 1.f};
-  if (grp.call.stats) {
-    if (grp.call.stats->finite != 1.f) return;
-    s.scale = grp.call.stats->scale;
-  }
+  Scalars s;
+  if (!scalars(grp.call, s)) return;
   const int block = grp.call.block0 + span_of_block();
   const int i = tensor_of_block(grp.begin, grp.call.count, block);
   const AdamWQ8Tensor& p = grp.t[i];
-  s.keep = p.keep;
+  s.keep = __builtin_fmaf(-s.lr, p.decay, 1.f);
   const int64_t first = (int64_t)(block - grp.begin[i]) * kSpanQ8, rest = p.count - first;
   const int n = rest < kSpanQ8 ? (int)rest : kSpanQ8;
   const int types = grp.types[i] + (p.master ? 4 : 0);
@@ -401,6 +404,14 @@ __global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const AdamWQ8Gr
   }
 }
 
+// One thread: the corrections of a step are two powers in 64 bits, which the threads of the step itself would each repeat.
+__global__ void adamw_tick_kernel(AdamWClock* clock, double beta1, double beta2, const GradStats* stats) {
+  if (stats && stats->finite != 1.f) return;
+  const int64_t t = ++clock->t;
+  clock->inv_c1 = (float)(1.0 / (1.0 - pow(beta1, (double)t)));
+  clock->inv_c2 = (float)(1.0 / (1.0 - pow(beta2, (double)t)));
+}
+
 // Spans of the list's tensors and the launches over them: one, unless a launch cannot have so many workgroups.
 template <class Group, class Kernel> hipError_t launch_spans(Group& g, int64_t span, Kernel kernel, hipStream_t stream) {
   int64_t blocks = 0;
@@ -420,6 +431,11 @@ template <class Group, class Kernel> hipError_t launch_spans(Group& g, int64_t s
 }
 
 }  // namespace
+
+hipError_t launch_adamw_tick(AdamWClock* clock, float beta1, float beta2, const GradStats* stats, hipStream_t stream) {
+  hipLaunchKernelGGL(adamw_tick_kernel, dim3(1), dim3(1), 0, stream, clock, (double)beta1, (double)beta2, stats);
+  return hipGetLastError();
+}
 
 hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream) {
   if (g.call.count > kAdamWTensors) return hipErrorInvalidValue;

@@ -13,6 +13,13 @@ struct GradStats {
   float norm, scale, finite, reserved;
 };
 
+// Step count, learning rate and bias corrections on the device (galore_adamw_clock).
+struct AdamWClock {
+  int64_t t;
+  float lr, inv_c1, inv_c2, reserved;
+};
+hipError_t launch_adamw_tick(AdamWClock* clock, float beta1, float beta2, const GradStats* stats, hipStream_t stream);
+
 // A kernel's arguments stay under 4 KiB: so many tensors per launch.
 constexpr int kAdamWTensors = 56;
 constexpr int kAdamWQ8Tensors = 44;
@@ -26,7 +33,7 @@ struct AdamWTensor {
   float* master;   // NULL: W is its own master
   int64_t count;   // rows * cols
   int32_t cols, ldw, ldg;
-  float keep;      // 1 - lr * weight decay
+  float decay;     // weight decay
 };
 
 struct AdamWQ8Tensor {
@@ -39,11 +46,12 @@ struct AdamWQ8Tensor {
   float* master;
   int64_t count;
   int32_t cols, ldw, ldg;
-  float keep;
+  float decay;
 };
 
 struct AdamWCall {
   const GradStats* stats;  // NULL: gradients as they are
+  const AdamWClock* clock; // NULL: lr and the corrections below
   float beta1, beta2, eps, lr;
   float inv_c1, inv_c2;    // 1 / (1 - beta^k)
   int32_t count;

@@ -9,7 +9,9 @@
 using namespace galore;
 using namespace galore::api;
 
-static_assert(sizeof(galore_grad_stats) == sizeof(GradStats), "the device's view of the statistics");
+static_assert(sizeof(galore_grad_stats) == sizeof(GradStats) && sizeof(galore_adamw_clock) == sizeof(AdamWClock) &&
+                  offsetof(galore_adamw_clock, lr) == offsetof(AdamWClock, lr),
+              "the device's view of the ABI's structs");
 
 namespace {
 
@@ -49,6 +51,16 @@ galore_status fail_twice(const char* what, int i) {
 
 galore_status check_stats(const galore_grad_stats* stats) {
   if (reinterpret_cast<uintptr_t>(stats) & 15) return fail(nullptr, GALORE_ERR_ALIGN, "stats must be 16-byte aligned");
+  return GALORE_OK;
+}
+
+galore_status check_clock(const galore_adamw_clock* clock) {
+  if (reinterpret_cast<uintptr_t>(clock) & 7) return fail(nullptr, GALORE_ERR_ALIGN, "clock must be 8-byte aligned");
+  return GALORE_OK;
+}
+
+galore_status check_betas(float beta1, float beta2) {
+  if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "betas must lie in [0, 1)");
   return GALORE_OK;
 }
 
@@ -104,15 +116,17 @@ galore_status fill_grads(const galore_tensor* G, int32_t count, std::vector<Grad
 extern "C" {
 
 galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count, float beta1,
-                           float beta2, float eps, float lr, int64_t k, const galore_grad_stats* stats, void* hip_stream) try {
+                           float beta2, float eps, float lr, int64_t k, const galore_adamw_clock* clock, const galore_grad_stats* stats,
+                           void* hip_stream) try {
   if (count < 0) return fail(nullptr, GALORE_ERR_INVALID_ARG, "count %d < 0", count);
   if (count > 0 && (!W || !G || !S)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "W / G / S is NULL");
-  if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) || !(eps >= 0.f))
-    return fail(nullptr, GALORE_ERR_INVALID_ARG, "betas / eps out of range");
-  if (!std::isfinite(lr)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "lr is not finite");
-  if (k < 1) return fail(nullptr, GALORE_ERR_INVALID_ARG, "k must be >= 1");
-  galore_status s = check_stats(stats);
-  if (s) return s;
+  galore_status s;
+  if ((s = check_betas(beta1, beta2)) || (s = check_stats(stats)) || (s = check_clock(clock))) return s;
+  if (!(eps >= 0.f)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "eps out of range");
+  if (!clock) {
+    if (!std::isfinite(lr)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "lr is not finite");
+    if (k < 1) return fail(nullptr, GALORE_ERR_INVALID_ARG, "k must be >= 1");
+  }
   Addresses written((size_t)count * 6);
   for (int32_t i = 0; i < count; ++i) {
     const galore_adamw_state& st = S[i];
@@ -144,9 +158,13 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
 
   AdamWCall call{};
   call.stats = reinterpret_cast<const GradStats*>(stats);
-  call.beta1 = beta1; call.beta2 = beta2; call.eps = eps; call.lr = lr;
-  call.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)k)));
-  call.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)beta2, (double)k)));
+  call.clock = reinterpret_cast<const AdamWClock*>(clock);
+  call.beta1 = beta1; call.beta2 = beta2; call.eps = eps;
+  if (!clock) {
+    call.lr = lr;
+    call.inv_c1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)k)));
+    call.inv_c2 = (float)(1.0 / (1.0 - std::pow((double)beta2, (double)k)));
+  }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipSuccess;
   AdamWGroup g{};
@@ -158,7 +176,7 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
     t.master = static_cast<float*>(S[i].master.data);
     t.count = W[i].rows * W[i].cols;
     t.cols = (int32_t)W[i].cols; t.ldw = run_ld(W[i]); t.ldg = run_ld(G[i]);
-    t.keep = (float)(1.0 - (double)lr * (double)S[i].weight_decay);
+    t.decay = S[i].weight_decay;
   };
   for (int32_t i = 0; i < count && e == hipSuccess; ++i) {
     if (S[i].m.dtype == GALORE_U8) {
@@ -181,6 +199,15 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
   return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "AdamW launch");
 } catch (...) {
   return fail(nullptr, GALORE_ERR_INVALID_ARG, "out of host memory");
+}
+
+galore_status galore_adamw_tick(galore_adamw_clock* clock, float beta1, float beta2, const galore_grad_stats* stats, void* hip_stream) {
+  if (!clock) return fail(nullptr, GALORE_ERR_INVALID_ARG, "clock is NULL");
+  galore_status s;
+  if ((s = check_betas(beta1, beta2)) || (s = check_stats(stats)) || (s = check_clock(clock))) return s;
+  const hipError_t e = launch_adamw_tick(reinterpret_cast<AdamWClock*>(clock), beta1, beta2, reinterpret_cast<const GradStats*>(stats),
+                                         static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "AdamW tick launch");
 }
 
 galore_status galore_grad_norm_workspace_bytes(int32_t count, size_t* out_bytes) {

@@ -28,14 +28,14 @@ class Call:
         self.S = [gb.galore_adamw_state(t(moments), t(moments), t(F32, 1, blocks) if moments == U8 else NONE,
                                         t(F32, 1, blocks) if moments == U8 else NONE, t(F32) if master else NONE, 0.01) for _ in range(n)]
         self.scalars = dict(beta1=0.9, beta2=0.999, eps=1e-8, lr=1e-3, k=1)
-        self.stats, self.count = None, n
+        self.stats, self.count, self.clock = None, n, None
 
     def status(self, **kw):
         a = dict(self.scalars, **kw)
         n = len(self.W)
         arr = lambda items, typ: None if items is None else (typ * n)(*items)
         return gb.lib().galore_adamw(arr(self.W, T), arr(self.G, T), arr(self.S, gb.galore_adamw_state), self.count,
-                                     a["beta1"], a["beta2"], a["eps"], a["lr"], a["k"], self.stats, None)
+                                     a["beta1"], a["beta2"], a["eps"], a["lr"], a["k"], self.clock, self.stats, None)
 
 
 def test_adamw_refuses_bad_scalars():
@@ -50,12 +50,18 @@ def test_adamw_refuses_bad_scalars():
     assert c.status() == 1
     c = Call(); c.stats = BASE + 4
     assert c.status() == 5
+    c = Call(); c.clock = BASE + 4
+    assert c.status() == 5
+    tick = gb.lib().galore_adamw_tick
+    assert tick(None, 0.9, 0.999, None, None) == 1
+    assert tick(BASE, 1.0, 0.999, None, None) == 1 and tick(BASE, 0.9, float("nan"), None, None) == 1
+    assert tick(BASE + 4, 0.9, 0.999, None, None) == 5 and tick(BASE, 0.9, 0.999, BASE + 8, None) == 5
 
 
 def test_adamw_refuses_missing_and_misshapen_tensors():
     L = gb.lib()
-    assert L.galore_adamw(None, None, None, 1, 0.9, 0.999, 1e-8, 1e-3, 1, None, None) == 1
-    assert L.galore_adamw(None, None, None, 0, 0.9, 0.999, 1e-8, 1e-3, 1, None, None) == 0      # an empty list is a step
+    assert L.galore_adamw(None, None, None, 1, 0.9, 0.999, 1e-8, 1e-3, 1, None, None, None) == 1
+    assert L.galore_adamw(None, None, None, 0, 0.9, 0.999, 1e-8, 1e-3, 1, None, None, None) == 0      # an empty list is a step
     for field in ("W", "G"):
         c = Call(); getattr(c, field)[1].data = None
         assert c.status() == 1, field
@@ -168,6 +174,8 @@ def test_python_face_refuses_what_the_library_cannot_see():
         gb.GaLoreAdamW([], weight_decay=[0.1], device="cpu")
     with pytest.raises(ValueError):
         gb._stats_ptr(torch.zeros(4))
+    with pytest.raises(ValueError):
+        gb._clock_ptr(torch.zeros(24, dtype=torch.uint8))
     with pytest.raises(ValueError):
         gb.galore_adamw((T * 1)(), (T * 2)(), [], 0.9, 0.999, 1e-8, 1e-3, 1)
 

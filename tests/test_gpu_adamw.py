@@ -374,6 +374,57 @@ def test_captured_calls_replay(moments):
             assert torch.equal(x, y), i
 
 
+@pytest.mark.parametrize("moments", ["f32", "q8"])
+def test_replays_count_their_steps_on_the_device(moments):
+    # norm, tick and AdamW captured once: every replay is the next step with the current rate, and a gradient that is not
+    # finite leaves a step out and does not count; against eager calls with host counts
+    torch.manual_seed(1)
+    W = [torch.randn(33, 260, device="cuda"), torch.randn(900, device="cuda").bfloat16()]
+    G = [torch.zeros_like(w) for w in W]
+    Wr = [w.clone() for w in W]
+    opt = gb.GaLoreAdamW(W, moments=moments, weight_decay=0.1, capturable=True)
+    ref = gb.GaLoreAdamW(Wr, moments=moments, weight_decay=0.1)
+    norm, norm_r = gb.GaLoreGradNorm(2, max_norm=1.0), gb.GaLoreGradNorm(2, max_norm=1.0)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        opt.step(W, G, stats=norm.measure(G))
+    assert opt.count() == 0
+    for i in range(7):
+        torch.manual_seed(40 + i)
+        for g in G:
+            g.copy_(torch.randn_like(g))
+        if i == 3:
+            G[1][5] = float("nan")
+        opt.set_lr(1e-2 / (i + 1))
+        graph.replay()
+        if i != 3:
+            ref.step(Wr, G, 1e-2 / (i + 1), norm_r.measure(G))
+        torch.cuda.synchronize()
+        assert opt.count() == ref.t
+        for x, y in zip(W + [opt.M_flat, opt.V_flat], Wr + [ref.M_flat, ref.V_flat]):
+            assert torch.equal(x, y), i
+    opt.step(W, G, 1e-3)                                                  # eager, behind the replays
+    ref.step(Wr, G, 1e-3)
+    assert opt.count() == ref.t == 7 and all(torch.equal(x, y) for x, y in zip(W, Wr))
+
+
+@pytest.mark.parametrize("beta1,beta2", [(0.9, 0.999), (0.0, 0.95), (0.99, 0.99999)])
+def test_bias_corrections_of_the_device_clock(beta1, beta2):
+    clock = torch.zeros(24, dtype=torch.uint8, device="cuda")
+    for t in (0, 1, 2, 9, 99, 4567, 10 ** 6, 1 << 40):
+        clock[:8].view(torch.int64).fill_(t)
+        gb.galore_adamw_tick(clock, beta1, beta2)
+        assert int(clock[:8].view(torch.int64)) == t + 1
+        got = clock[12:20].view(torch.float32).double().cpu().numpy()
+        want = [1.0 / (1.0 - f32(b) ** (t + 1)) for b in (beta1, beta2)]
+        # rounded once from 64 bits: half a step, and what 64 bits lose where 1 - b^t cancels (at most 2^17 times 2^-52)
+        assert np.all(np.abs(got - want) <= (U + 2.0 ** -35) * np.asarray(want)), t
+    clock.zero_()
+    gb.galore_adamw_tick(clock, 0.9, 0.999, _stats(1.0, finite=0.0))
+    assert not clock.any()
+
+
 def test_calls_run_on_the_current_stream():
     w, g = torch.zeros(1 << 20, device="cuda"), torch.zeros(1 << 20, device="cuda")
     opt = gb.GaLoreAdamW([w], eps=0.0)
