@@ -441,8 +441,9 @@ galore_status galore_adamw_tick(galore_adamw_clock* clock, float beta1, float be
  *     W <- (1 - lr*weight_decay) W - lr (m / (1-beta1^k)) / (sqrt(v / (1-beta2^k)) + eps)
  * in fp32, W rounded once.  With a clock (else NULL), lr and k are those on the device and the arguments are not used.
  * If stats->finite is not 1 the call leaves every tensor as it was (a k of the caller's should then be used once more).
- * Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their
- * block) non-finite.
+ * Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their block) non-finite.
+ * The second moment is formed in fp32: entries of g beyond about 1e19 in magnitude overflow it (their weight then only
+ * decays), as squares below 1e-38 vanish in it.
  * One launch for up to 56 tensors with fp32 moments, or up to 44 with 8-bit ones.
  * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address, or a gradient
  * does at that of one of them; tensors that overlap otherwise are not detected and must not be passed. */

@@ -5,6 +5,7 @@ PyTorch is used for device memory and for the current HIP stream.  There is no f
 if the library is missing this module raises.
 """
 import ctypes
+import functools
 import os
 
 import torch  # also loads the HIP runtime the library binds to
@@ -483,34 +484,62 @@ class GaLoreAdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(weights)
         if len(decay) != len(weights):
             raise ValueError("one weight_decay per tensor")
-        for w in weights:
-            param_desc(w)  # refuses what a step could not take
+        descs = [param_desc(w) for w in weights]  # refuses what a step could not take
         starts, total = [], 0
-        for w in weights:
+        for d in descs:
             starts.append(total)
-            total += -(-w.numel() // self._ALIGN) * self._ALIGN
+            total += -(-d.rows * d.cols // self._ALIGN) * self._ALIGN
+        self._places = [(s, w.shape, w.numel()) for s, w in zip(starts, weights)]
+        self._has_master = [master and d.dtype == GALORE_BF16 for d in descs]
         q8 = moments == "q8"
-        code = torch.uint8 if q8 else torch.float32
+        code, dt, size = (torch.uint8, GALORE_U8, 1) if q8 else (torch.float32, GALORE_F32, 4)
         self.M_flat, self.V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
         self.M_scale_flat, self.V_scale_flat = ((torch.zeros(total // self._ALIGN, device=device) for _ in range(2)) if q8 else (None, None))
         self.master_flat = torch.zeros(total, device=device) if master else None
-        cut = lambda flat: [flat[s:s + w.numel()].view(w.shape) for s, w in zip(starts, weights)]
-        blocks = lambda flat: [flat[s // self._ALIGN:-(-(s + w.numel()) // self._ALIGN)] for s, w in zip(starts, weights)]
-        self.M, self.V = cut(self.M_flat), cut(self.V_flat)
-        self.M_scale, self.V_scale = (blocks(self.M_scale_flat), blocks(self.V_scale_flat)) if q8 else ([], [])
-        self.master = [m if w.dtype == torch.bfloat16 else None for m, w in zip(cut(self.master_flat), weights)] if master else [None] * len(weights)
-        none = galore_tensor(None, 0, 0, 0, GALORE_F32)
-        states = []
         for i, w in enumerate(weights):
-            if self.master[i] is not None:
+            if self._has_master[i]:
                 self.master[i].copy_(w.detach())
-            d = param_desc(w)
-            like = lambda t: galore_tensor(t.data_ptr(), d.rows, d.cols, d.cols, _DTYPES[t.dtype])
-            states.append(galore_adamw_state(like(self.M[i]), like(self.V[i]), param_desc(self.M_scale[i]) if q8 else none,
-                                             param_desc(self.V_scale[i]) if q8 else none,
-                                             like(self.master[i]) if self.master[i] is not None else none, decay[i]))
-        self._states = (galore_adamw_state * len(states))(*states)
+        base = lambda t: t.data_ptr() if t is not None else 0
+        m, v, ms, vs, x = map(base, (self.M_flat, self.V_flat, self.M_scale_flat, self.V_scale_flat, self.master_flat))
+        none = galore_tensor(None, 0, 0, 0, GALORE_F32)
+        self._states = (galore_adamw_state * len(descs))()
+        for st, s, d, decays, has_master in zip(self._states, starts, descs, decay, self._has_master):
+            at = lambda p, size, dt: galore_tensor(p + s * size, d.rows, d.cols, d.cols, dt)
+            st.m, st.v, st.weight_decay = at(m, size, dt), at(v, size, dt), decays
+            if q8:
+                blocks = -(-d.rows * d.cols // self._ALIGN)
+                st.m_scale, st.v_scale = (galore_tensor(p + s // self._ALIGN * 4, 1, blocks, blocks, GALORE_F32) for p in (ms, vs))
+            st.master = at(x, 4, GALORE_F32) if has_master else none
         self.clock = torch.zeros(ctypes.sizeof(galore_adamw_clock), dtype=torch.uint8, device=device) if capturable else None
+
+    # The state of every tensor, as views of the flat buffers (which are what a checkpoint saves, with the step count).
+    # After a weight was replaced (loaded) the caller copies it to its master as well.
+    def _views(self, flat):
+        return [flat[s:s + n].view(shape) for s, shape, n in self._places]
+
+    def _scale_views(self, flat):
+        return [flat[s // self._ALIGN:-(-(s + n) // self._ALIGN)] for s, _, n in self._places] if flat is not None else []
+
+    @functools.cached_property
+    def M(self):
+        return self._views(self.M_flat)
+
+    @functools.cached_property
+    def V(self):
+        return self._views(self.V_flat)
+
+    @functools.cached_property
+    def M_scale(self):
+        return self._scale_views(self.M_scale_flat)
+
+    @functools.cached_property
+    def V_scale(self):
+        return self._scale_views(self.V_scale_flat)
+
+    @functools.cached_property
+    def master(self):
+        views = self._views(self.master_flat) if self.master_flat is not None else [None] * len(self._places)
+        return [x if has else None for x, has in zip(views, self._has_master)]
 
     def set_lr(self, lr):
         """capturable: the learning rate of the steps from here on (ordered by the current stream)."""
