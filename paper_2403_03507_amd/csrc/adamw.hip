@@ -39,53 +39,30 @@ __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { ret
 
 template <class TW, class TG, bool MASTER>
 __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& s, int64_t first, int n) {
-  typedef ListF32<4> f4;
-  const int o = threadIdx.x * 4;
-  if (o >= n) return;
-  float* __restrict__ M = p.M + first;
-  float* __restrict__ V = p.V + first;
-  float* __restrict__ X = MASTER ? p.master + first : nullptr;
-  TW* __restrict__ W = static_cast<TW*>(p.W);
-  const TG* __restrict__ G = static_cast<const TG*>(p.G);
-  int64_t aw = o, ag = o;
-  uint32_t left = 4;
-  const bool dense = p.ldw == p.cols && p.ldg == p.cols;
-  if (dense) {
-    W += first; G += first;
-  } else {
-    const RowWalk::Place at = RowWalk(first, p.cols).at(o);
-    aw = at.offset(p.ldw); ag = at.offset(p.ldg); left = at.left;
-  }
-  if (o + 4 <= n && left >= 4) {
-    const f4 g = list_load<4>(G + ag);
-    f4 m = list_load<4>(M + o), v = list_load<4>(V + o);
-    f4 w = MASTER ? list_load<4>(X + o) : list_load<4>(W + aw);
+  const int o = threadIdx.x * 4, have = n - o;
+  if (have <= 0) return;
+  float* M = p.M + first;
+  float* V = p.V + first;
+  float* X = MASTER ? p.master + first : nullptr;
+  TW* W = static_cast<TW*>(p.W);
+  const TG* G = static_cast<const TG*>(p.G);
+  const RowWalk::Place run = RowWalk::Place::in_run(o);
+  RowWalk::Place at = run;
+  if (p.ldw == p.cols && p.ldg == p.cols) { W += first; G += first; }
+  else at = RowWalk(first, p.cols).at(o);
+  ListF32<4> g = row_load<4>(G, p.ldg, p.cols, at, have), m = row_load<4>(M, 0, 0, run, have), v = row_load<4>(V, 0, 0, run, have);
+  ListF32<4> w = MASTER ? row_load<4>(X, 0, 0, run, have) : row_load<4>(W, p.ldw, p.cols, at, have);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float me = m[e], ve = v[e];
-      const float ne = adam_entry(s.scale * g[e], me, ve, s.beta1, s.beta2, s.eps, s.inv_c1, s.inv_c2);
-      m[e] = me; v[e] = ve;
-      w[e] = apply(w[e], ne, s);
-    }
-    list_store<4>(M + o, m);
-    list_store<4>(V + o, v);
-    if (MASTER) list_store<4>(X + o, w);
-    list_store<4>(W + aw, w);
-    return;
+  for (int e = 0; e < 4; ++e) {
+    float me = m[e], ve = v[e];
+    const float ne = adam_entry(s.scale * g[e], me, ve, s.beta1, s.beta2, s.eps, s.inv_c1, s.inv_c2);
+    m[e] = me; v[e] = ve;
+    w[e] = apply(w[e], ne, s);
   }
-  // the end of the tensor, or of a row with a gap behind it
-  const RowWalk walk(dense ? 0 : first, p.cols);
-#pragma unroll 1
-  for (int e = o; e < o + 4 && e < n; ++e) {
-    int64_t we = e, ge = e;
-    if (!dense) { const RowWalk::Place at = walk.at(e); we = at.offset(p.ldw); ge = at.offset(p.ldg); }
-    float m = M[e], v = V[e];
-    const float ne = adam_entry(s.scale * (float)G[ge], m, v, s.beta1, s.beta2, s.eps, s.inv_c1, s.inv_c2);
-    M[e] = m; V[e] = v;
-    const float w = apply(MASTER ? X[e] : (float)W[we], ne, s);
-    if (MASTER) X[e] = w;
-    W[we] = (TW)w;
-  }
+  row_store<4>(M, 0, 0, run, have, m);
+  row_store<4>(V, 0, 0, run, have, v);
+  if (MASTER) row_store<4>(X, 0, 0, run, have, w);
+  row_store<4>(W, p.ldw, p.cols, at, have, w);
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup grp) {
@@ -224,38 +201,6 @@ struct LaneQ8 {
   bool simple;         // a whole block of a tensor without gaps between its rows
 };
 
-// Four elements from place `at` on, `n` of them (the others count as zero): rows may lie apart.
-template <class T> __device__ __forceinline__ ListF32<4> load_group(const T* p, int32_t ld, const RowWalk& walk, const RowWalk::Place& at, int n) {
-  ListF32<4> x = 0.f;
-  if (n <= 0) return x;
-  p += at.offset(ld);
-  if (n >= 4 && at.left >= 4) return list_load<4>(p);
-  const int64_t gap = (int64_t)ld - walk.cols;   // a row is at least one element long: count the ends that are passed
-  int64_t skip = 0;
-  uint32_t left = at.left;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (left == 0) { skip += gap; left = walk.cols; }
-    if (e < n) x[e] = (float)p[e + skip];
-    --left;
-  }
-  return x;
-}
-template <class T> __device__ __forceinline__ void store_group(T* p, int32_t ld, const RowWalk& walk, const RowWalk::Place& at, int n, ListF32<4> x) {
-  if (n <= 0) return;
-  p += at.offset(ld);
-  if (n >= 4 && at.left >= 4) { list_store<4>(p, x); return; }
-  const int64_t gap = (int64_t)ld - walk.cols;
-  int64_t skip = 0;
-  uint32_t left = at.left;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (left == 0) { skip += gap; left = walk.cols; }
-    if (e < n) p[e + skip] = (T)x[e];
-    --left;
-  }
-}
-
 template <class TW, class TG, bool MASTER, bool ROW>
 __device__ __forceinline__ void load_q8(const AdamWQ8Tensor& p, const LaneQ8& l, ListF32<8>& g, ListF32<8>& w) {
   typedef typename std::conditional<MASTER, float, TW>::type TX;
@@ -281,8 +226,8 @@ __device__ __forceinline__ void load_q8(const AdamWQ8Tensor& p, const LaneQ8& l,
     }
     const RowWalk::Place p1 = walk.at(l.at1);
     const int32_t ldx = MASTER ? p.cols : p.ldw;
-    g0 = load_group(G, p.ldg, walk, p0, l.n0); g1 = load_group(G, p.ldg, walk, p1, l.n1);
-    w0 = load_group(X, ldx, walk, p0, l.n0); w1 = load_group(X, ldx, walk, p1, l.n1);
+    g0 = row_load<4>(G, p.ldg, p.cols, p0, l.n0); g1 = row_load<4>(G, p.ldg, p.cols, p1, l.n1);
+    w0 = row_load<4>(X, ldx, p.cols, p0, l.n0); w1 = row_load<4>(X, ldx, p.cols, p1, l.n1);
   }
   g = __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7);
   w = __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -315,11 +260,11 @@ __device__ __forceinline__ void store_q8(const AdamWQ8Tensor& p, const LaneQ8& l
   }
   const RowWalk::Place p1 = walk.at(l.at1);
   if (MASTER) {
-    store_group(p.master, p.cols, walk, p0, l.n0, w0);
-    store_group(p.master, p.cols, walk, p1, l.n1, w1);
+    row_store<4>(p.master, p.cols, p.cols, p0, l.n0, w0);
+    row_store<4>(p.master, p.cols, p.cols, p1, l.n1, w1);
   }
-  store_group(W, p.ldw, walk, p0, l.n0, w0);
-  store_group(W, p.ldw, walk, p1, l.n1, w1);
+  row_store<4>(W, p.ldw, p.cols, p0, l.n0, w0);
+  row_store<4>(W, p.ldw, p.cols, p1, l.n1, w1);
 }
 
 typedef uint32_t q_u32x2 __attribute__((ext_vector_type(2)));

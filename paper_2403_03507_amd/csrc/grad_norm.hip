@@ -42,7 +42,6 @@ template <class T, bool CACHED> __device__ __forceinline__ double squares(const 
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = __builtin_fma((double)g[e], (double)g[e], sum[e]);
   };
-  const auto one = [&](T x) { sum[0] = __builtin_fma((double)(float)x, (double)(float)x, sum[0]); };
   if (p.ld == p.cols) {
     constexpr int kStep = kNormThreads * N;
     G += first;
@@ -52,18 +51,13 @@ template <class T, bool CACHED> __device__ __forceinline__ double squares(const 
       add(a);
       add(b);
     }
-    for (; o < n; o += kStep) {
-      if (o + N <= n) add(list_load<N, CACHED>(G + o));
-      else for (int64_t e = o; e < n; ++e) one(G[e]);
-    }
+    for (; o < n; o += kStep) add(row_load<N, CACHED>(G + o, 0, 0, RowWalk::Place::in_run(0), n - o < N ? (int)(n - o) : N));
   } else {
     for (int64_t base = 0; base < n; base += kPiece) {
       const RowWalk walk(first + base, p.cols);
       const int len = n - base < kPiece ? (int)(n - base) : kPiece;
       for (int o = threadIdx.x * N; o < len; o += kNormThreads * N) {
-        const RowWalk::Place at = walk.at(o);
-        if (o + N <= len && at.left >= N) add(list_load<N, CACHED>(G + at.offset(p.ld)));
-        else for (int e = o; e < o + N && e < len; ++e) one(G[walk.at(e).offset(p.ld)]);
+        add(row_load<N, CACHED>(G, p.ld, p.cols, walk.at(o), len - o));
       }
     }
   }
@@ -117,17 +111,9 @@ template <class T> __device__ __forceinline__ void scale_span(const GradTensor& 
   const RowWalk walk(first, p.cols);
   for (int o = threadIdx.x * N; o < n; o += kStep) {
     const RowWalk::Place at = walk.at(o);
-    if (o + N <= n && at.left >= N) {
-      T* x = G + at.offset(p.ld);
-      ListF32<N> g = 0.f;
-      if (!zero) g = list_load<N>(x) * c;
-      list_store<N>(x, g);
-    } else {
-      for (int e = o; e < o + N && e < n; ++e) {
-        T& x = G[walk.at(e).offset(p.ld)];
-        x = zero ? (T)0.f : (T)((float)x * c);
-      }
-    }
+    ListF32<N> g = 0.f;
+    if (!zero) g = row_load<N>(G, p.ld, p.cols, at, n - o) * c;
+    row_store<N>(G, p.ld, p.cols, at, n - o, g);
   }
 }
 

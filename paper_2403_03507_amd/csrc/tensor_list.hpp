@@ -45,6 +45,8 @@ struct RowWalk {
   struct Place {
     int64_t row;
     uint32_t col, left;   // left: elements of the row from this one on
+    // element o of a run without gaps, counted from where the run starts
+    static __device__ __forceinline__ Place in_run(int o) { return Place{0, (uint32_t)o, 0x7FFFFFFFu}; }
     __device__ __forceinline__ int64_t offset(int32_t ld) const { return row * ld + col; }
   };
   __device__ __forceinline__ Place at(int o) const {
@@ -75,6 +77,37 @@ template <int N, bool CACHED = false, class T> __device__ __forceinline__ ListF3
 template <int N, class T> __device__ __forceinline__ void list_store(T* p, ListF32<N> x) {
   typedef typename ListVec<T, N>::type V;
   __builtin_nontemporal_store(__builtin_convertvector(x, V), reinterpret_cast<V*>(p));
+}
+
+// N elements from place `at` on, the first n of which the tensor has (the others count as zero): rows of `cols` elements
+// may lie apart.  Past a row's end the offset grows by the gap: no further division, and no load waits for another.
+template <int N, bool CACHED = false, class T>
+__device__ __forceinline__ ListF32<N> row_load(const T* p, int32_t ld, int32_t cols, const RowWalk::Place& at, int n) {
+  p += at.offset(ld);
+  if (n >= N && at.left >= N) return list_load<N, CACHED>(p);
+  ListF32<N> x = 0.f;
+  int64_t skip = 0;
+  uint32_t left = at.left;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (left == 0) { skip += ld - cols; left = cols; }
+    if (e < n) x[e] = (float)p[e + skip];
+    --left;
+  }
+  return x;
+}
+template <int N, class T>
+__device__ __forceinline__ void row_store(T* p, int32_t ld, int32_t cols, const RowWalk::Place& at, int n, ListF32<N> x) {
+  p += at.offset(ld);
+  if (n >= N && at.left >= N) { list_store<N>(p, x); return; }
+  int64_t skip = 0;
+  uint32_t left = at.left;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (left == 0) { skip += ld - cols; left = cols; }
+    if (e < n) p[e + skip] = (T)x[e];
+    --left;
+  }
 }
 
 }  // namespace galore
