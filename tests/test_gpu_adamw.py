@@ -336,6 +336,33 @@ def test_more_than_2_to_the_31_elements(moments, gdt):
     assert abs(float(norm.measure([G])[0]) - 0.5 * total) <= 2.0 ** -7 * total
 
 
+@pytest.mark.parametrize("moments,rows,cols", [("f32", (1 << 16) + 1, (1 << 16) + 4), ("q8", (1 << 17) + 1, (1 << 16) + 4)])
+def test_more_elements_than_one_launch_takes(moments, rows, cols):
+    # 2^23 workgroups of 512 (8-bit moments: 1024) elements are one launch; rows on both sides of that, and the last one
+    if torch.cuda.mem_get_info()[0] < 72 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    split = (1 << 23) * (512 if moments == "f32" else 1024)
+    assert rows * cols > split
+    W = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    G = torch.zeros_like(W)
+    at = [0, split // cols - 1, split // cols, split // cols + 1, rows - 1]
+    gen = torch.Generator("cuda").manual_seed(2)
+    for r in at:
+        W[r] = torch.randn(cols, generator=gen, device="cuda").bfloat16()
+        G[r] = torch.randn(cols, generator=gen, device="cuda").bfloat16()
+    W0, opt = W[at].clone(), gb.GaLoreAdamW([W], moments=moments, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD)
+    opt.step([W], [G], LR)
+    torch.cuda.synchronize()
+    z = np.zeros((1, cols))
+    for j, r in enumerate(at):
+        (w1, _, _), (dw, _, _) = _bounds(to64(W0[j:j + 1]), to64(G[r:r + 1]), z, z, 1, 1.0, WD)
+        _within(to64(W[r:r + 1]), w1, dw, torch.bfloat16)
+        W[r] = 0
+    assert int(torch.count_nonzero(W)) == 0
+    del W, G, opt
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("moments", ["f32", "q8"])
 def test_captured_calls_replay(moments):
     # norm, scaling of one part, AdamW of the other, captured once and replayed between eager work; the graph keeps its k

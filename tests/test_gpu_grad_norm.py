@@ -65,6 +65,28 @@ def test_norm_of_more_than_the_cache_holds():
     assert abs(float(stats[0]) - total ** 0.5) <= HALF * total ** 0.5
 
 
+def test_scaling_of_more_than_one_launch_takes():
+    # 2^23 workgroups of 2048 bf16 elements are one launch
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    n = (1 << 34) + 70000
+    G = torch.zeros(n // 10000, 10000, dtype=torch.bfloat16, device="cuda")
+    rows = [0, (1 << 34) // 10000, G.shape[0] - 1]
+    for r in rows:
+        G[r] = r % 7 + 1
+    norm = gb.GaLoreGradNorm(1, max_norm=1.0)
+    total = 100.0 * sum((r % 7 + 1) ** 2 for r in rows) ** 0.5
+    stats = norm.measure([G])
+    assert abs(float(stats[0]) - total) <= HALF * total
+    norm.scale([G], torch.tensor([1.0, 0.5, 1.0, 0.0], device="cuda"))
+    for r in rows:
+        assert bool((G[r] == (r % 7 + 1) / 2).all())
+        G[r] = 0
+    assert int(torch.count_nonzero(G)) == 0
+    del G
+    torch.cuda.empty_cache()
+
+
 def test_more_gradients_than_the_workspace_is_for():
     norm = gb.GaLoreGradNorm(2)
     G = [torch.ones(4, device="cuda") for _ in range(200)]
