@@ -150,6 +150,8 @@ def param_desc(t):
     trailing dimensions of a contiguous tensor of rank 3 and more are one."""
     if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
         raise ValueError("need a tensor on the current device")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("need fp32 or bf16")
     if t.dim() < 2:
         if t.dim() == 1 and t.shape[0] > 1 and t.stride(0) != 1:
             raise ValueError("need a contiguous vector")

@@ -16,6 +16,9 @@
 namespace galore {
 namespace {
 
+// A stream that is bound by HBM: what counts is that neighbours in memory are in flight together.  So a thread takes one
+// group of elements and is done (262M bf16 weights, fp32 moments: workgroups of 256 over 8192 elements 1062 us, over 2048
+// 1029, over 1024 948, of 128 over 512 934, of 512 over 2048 985; two groups a thread 981).
 constexpr int kThreads = 128;
 constexpr int kSpan = 512;      // elements per workgroup: one group of 4 per thread
 constexpr int kSpanQ8 = 1024;   // 8 per thread
@@ -36,6 +39,9 @@ __device__ __forceinline__ bool scalars(const AdamWCall& c, Scalars& s) {
 __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { return __builtin_fmaf(-s.lr, n, s.keep * w); }
 
 // ---- fp32 moments ----------------------------------------------------------------------------------
+// 22 bytes per bf16 element, 28 with fp32 or master weights, each moved once and past the caches; bound by HBM: 262M bf16
+// weights 908 us (6.36 TB/s), 101M with master copies 442 (6.37), 30M fp32 131 (6.39).  Arithmetic (48 instructions per
+// element, IEEE square root and division among them) takes a third of that.
 
 template <class TW, class TG, bool MASTER>
 __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& s, int64_t first, int n) {
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup g
 // as much as the traffic: 64 additions or the like per element would take as long as the bytes do.  So first-moment codes
 // go through the hardware's e4m3 conversions, second-moment codes are cut from fp32 bits, and the square root and the
 // reciprocal of the update are the hardware's approximations of one unit in the last place (exact ones: 202M bf16 elements
-// 388 us instead of 331).
+// 388 us instead of 331).  Measured: 202M bf16 weights 326 us (6.2 TB/s), 60M fp32 154 (6.3).
 
 typedef float q_f32x2 __attribute__((ext_vector_type(2)));
 typedef short q_s16x2 __attribute__((ext_vector_type(2)));

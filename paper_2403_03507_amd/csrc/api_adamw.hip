@@ -18,7 +18,8 @@ namespace {
 constexpr int64_t kBlock = 256;   // elements under one scale of the 8-bit moments
 
 // No two of the addresses that a call writes may be the same (the same tensor twice in a list, one buffer for two states).
-// A table with open addressing: a call of a small list costs the host more than the GPU (201 addresses: 1 us, sorted 4).
+// A table with open addressing: a call on a small list costs the host more than the GPU (67 tensors: 6 us in all; 16 with the
+// addresses sorted).
 class Addresses {
  public:
   explicit Addresses(size_t most) {

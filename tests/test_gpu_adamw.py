@@ -305,6 +305,15 @@ def test_parameters_of_any_rank():
         gb.param_desc(torch.randn(8, device="cuda")[::2])
     with pytest.raises(ValueError):
         gb.param_desc(torch.randn(4, 6, 8, device="cuda").transpose(0, 1))
+    with pytest.raises(ValueError):
+        gb.param_desc(torch.randn(4, 6, device="cuda").t())
+    with pytest.raises(ValueError):
+        gb.param_desc(torch.zeros(4, 6, dtype=torch.float16, device="cuda"))
+    w = torch.ones(3, 4, device="cuda")
+    one = gb.GaLoreAdamW([w])
+    with pytest.raises(gb.GaloreError) as e:                                  # a broadcast gradient has no rows of its own
+        one.step([w], [torch.ones(1, 4, device="cuda").expand(3, 4)], LR)
+    assert e.value.status == 2 and one.t == 0 and bool((w == 1).all())
 
 
 @pytest.mark.parametrize("moments,gdt", [("q8", "bf16"), ("f32", "f32")])
