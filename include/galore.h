@@ -444,7 +444,8 @@ galore_status galore_adamw_tick(galore_adamw_clock* clock, float beta1, float be
  * Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their block) non-finite.
  * The second moment is formed in fp32: entries of g beyond about 1e19 in magnitude overflow it (their weight then only
  * decays), as squares below 1e-38 vanish in it.
- * One launch for up to 56 tensors with fp32 moments, or up to 44 with 8-bit ones.
+ * One launch for up to 89 tensors with fp32 moments, and one for up to 66 with 8-bit ones (56 and 44 if one of them has a
+ * master copy, gaps between rows of W or G, or 2^31 elements).
  * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address, or a gradient
  * does at that of one of them; tensors that overlap otherwise are not detected and must not be passed. */
 galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const galore_adamw_state* S, int32_t count,

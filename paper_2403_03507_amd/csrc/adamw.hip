@@ -1,5 +1,5 @@
-// AdamW (decoupled weight decay) over a list of tensors, one launch for up to 56 of them (44 with 8-bit moments): the
-// step of the parameters that GaLore leaves alone.  Per element, with g = scale * G (scale: the clip factor of
+// AdamW (decoupled weight decay) over a list of tensors, one launch for up to 89 of them (66 with 8-bit moments): the step
+// of the parameters that GaLore leaves alone.  Per element, with g = scale * G (scale: the clip factor of
 // galore_grad_norm, or 1):
 //     m = b1 m + (1-b1) g ;  v = b2 v + (1-b2) g^2 ;  n = (m / (1-b1^k)) / (sqrt(v / (1-b2^k)) + eps)
 //     W = (1 - lr wd) W - lr n
@@ -36,6 +36,20 @@ __device__ __forceinline__ bool scalars(const AdamWCall& c, Scalars& s) {
   return c.stats->finite == 1.f;
 }
 
+// What the short descriptions leave out.
+template <class Tensor> __device__ __forceinline__ float* master_of(const Tensor& p) {
+  if constexpr (std::is_same<decltype(p.count), int64_t>::value) return p.master;
+  else return nullptr;
+}
+struct Lengths {
+  int32_t cols, ldw, ldg;   // a row's length, and from one to the next in W and G
+  __device__ __forceinline__ bool run() const { return ldw == cols && ldg == cols; }
+};
+template <class Tensor> __device__ __forceinline__ Lengths lengths_of(const Tensor& p) {
+  if constexpr (std::is_same<decltype(p.count), int64_t>::value) return Lengths{p.cols, p.ldw, p.ldg};
+  else return Lengths{INT32_MAX, INT32_MAX, INT32_MAX};   // one row
+}
+
 __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { return __builtin_fmaf(-s.lr, n, s.keep * w); }
 
 // ---- fp32 moments ----------------------------------------------------------------------------------
@@ -43,21 +57,22 @@ __device__ __forceinline__ float apply(float w, float n, const Scalars& s) { ret
 // weights 908 us (6.36 TB/s), 101M with master copies 442 (6.37), 30M fp32 131 (6.39).  Arithmetic (48 instructions per
 // element, IEEE square root and division among them) takes a third of that.
 
-template <class TW, class TG, bool MASTER>
-__device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& s, int64_t first, int n) {
+template <class TW, class TG, bool MASTER, class Tensor>
+__device__ __forceinline__ void adamw_span(const Tensor& p, const Scalars& s, int64_t first, int n) {
   const int o = threadIdx.x * 4, have = n - o;
   if (have <= 0) return;
   float* M = p.M + first;
   float* V = p.V + first;
-  float* X = MASTER ? p.master + first : nullptr;
+  float* X = MASTER ? master_of(p) + first : nullptr;
   TW* W = static_cast<TW*>(p.W);
   const TG* G = static_cast<const TG*>(p.G);
+  const Lengths len = lengths_of(p);
   const RowWalk::Place run = RowWalk::Place::in_run(o);
   RowWalk::Place at = run;
-  if (p.ldw == p.cols && p.ldg == p.cols) { W += first; G += first; }
-  else at = RowWalk(first, p.cols).at(o);
-  ListF32<4> g = row_load<4>(G, p.ldg, p.cols, at, have), m = row_load<4>(M, 0, 0, run, have), v = row_load<4>(V, 0, 0, run, have);
-  ListF32<4> w = MASTER ? row_load<4>(X, 0, 0, run, have) : row_load<4>(W, p.ldw, p.cols, at, have);
+  if (len.run()) { W += first; G += first; }
+  else at = RowWalk(first, len.cols).at(o);
+  ListF32<4> g = row_load<4>(G, len.ldg, len.cols, at, have), m = row_load<4>(M, 0, 0, run, have), v = row_load<4>(V, 0, 0, run, have);
+  ListF32<4> w = MASTER ? row_load<4>(X, 0, 0, run, have) : row_load<4>(W, len.ldw, len.cols, at, have);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     float me = m[e], ve = v[e];
@@ -68,19 +83,19 @@ __device__ __forceinline__ void adamw_span(const AdamWTensor& p, const Scalars& 
   row_store<4>(M, 0, 0, run, have, m);
   row_store<4>(V, 0, 0, run, have, v);
   if (MASTER) row_store<4>(X, 0, 0, run, have, w);
-  row_store<4>(W, p.ldw, p.cols, at, have, w);
+  row_store<4>(W, len.ldw, len.cols, at, have, w);
 }
 
-__global__ __launch_bounds__(kThreads) void adamw_list_kernel(const AdamWGroup grp) {
+template <class List> __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const List grp) {
   Scalars s;
   if (!scalars(grp.call, s)) return;
   const int block = grp.call.block0 + span_of_block();
   const int i = tensor_of_block(grp.begin, grp.call.count, block);
-  const AdamWTensor& p = grp.t[i];
+  const auto& p = grp.t[i];
   s.keep = __builtin_fmaf(-s.lr, p.decay, 1.f);
   const int64_t first = (int64_t)(block - grp.begin[i]) * kSpan, rest = p.count - first;
   const int n = rest < kSpan ? (int)rest : kSpan;
-  const bool master = p.master != nullptr;
+  const bool master = master_of(p) != nullptr;
   switch (grp.types[i]) {
     case 0: adamw_span<float, float, false>(p, s, first, n); break;
     case 2: adamw_span<float, __bf16, false>(p, s, first, n); break;
@@ -207,10 +222,10 @@ struct LaneQ8 {
   bool simple;         // a whole block of a tensor without gaps between its rows
 };
 
-template <class TW, class TG, bool MASTER, bool ROW>
-__device__ __forceinline__ void load_q8(const AdamWQ8Tensor& p, const LaneQ8& l, ListF32<8>& g, ListF32<8>& w) {
+template <class TW, class TG, bool MASTER, bool ROW, class Tensor>
+__device__ __forceinline__ void load_q8(const Tensor& p, const LaneQ8& l, ListF32<8>& g, ListF32<8>& w) {
   typedef typename std::conditional<MASTER, float, TW>::type TX;
-  const TX* X = MASTER ? reinterpret_cast<const TX*>(p.master) : static_cast<const TX*>(p.W);
+  const TX* X = MASTER ? reinterpret_cast<const TX*>(master_of(p)) : static_cast<const TX*>(p.W);
   const TG* G = static_cast<const TG*>(p.G);
   ListF32<4> g0, g1, w0, w1;
   if (l.simple) {
@@ -223,30 +238,31 @@ __device__ __forceinline__ void load_q8(const AdamWQ8Tensor& p, const LaneQ8& l,
     g0 = list_load<4>(G + l.at0); g1 = list_load<4>(G + l.at1);
     w0 = list_load<4>(X + l.at0); w1 = list_load<4>(X + l.at1);
   } else {
-    const RowWalk walk(l.first, p.cols);
+    const Lengths len = lengths_of(p);
+    const RowWalk walk(l.first, len.cols);
     const RowWalk::Place p0 = walk.at(l.at0);
     if (ROW && l.n0 >= 8 && p0.left >= 8) {
-      g = list_load<8>(G + p0.offset(p.ldg));
-      w = list_load<8>(X + p0.offset(p.ldw));
+      g = list_load<8>(G + p0.offset(len.ldg));
+      w = list_load<8>(X + p0.offset(len.ldw));
       return;
     }
     const RowWalk::Place p1 = walk.at(l.at1);
-    const int32_t ldx = MASTER ? p.cols : p.ldw;
-    g0 = row_load<4>(G, p.ldg, p.cols, p0, l.n0); g1 = row_load<4>(G, p.ldg, p.cols, p1, l.n1);
-    w0 = row_load<4>(X, ldx, p.cols, p0, l.n0); w1 = row_load<4>(X, ldx, p.cols, p1, l.n1);
+    const int32_t ldx = MASTER ? len.cols : len.ldw;
+    g0 = row_load<4>(G, len.ldg, len.cols, p0, l.n0); g1 = row_load<4>(G, len.ldg, len.cols, p1, l.n1);
+    w0 = row_load<4>(X, ldx, len.cols, p0, l.n0); w1 = row_load<4>(X, ldx, len.cols, p1, l.n1);
   }
   g = __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7);
   w = __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-template <class TW, bool MASTER, bool ROW>
-__device__ __forceinline__ void store_q8(const AdamWQ8Tensor& p, const LaneQ8& l, const ListF32<8>& w) {
+template <class TW, bool MASTER, bool ROW, class Tensor>
+__device__ __forceinline__ void store_q8(const Tensor& p, const LaneQ8& l, const ListF32<8>& w) {
   TW* W = static_cast<TW*>(p.W);
   const ListF32<4> w0 = __builtin_shufflevector(w, w, 0, 1, 2, 3), w1 = __builtin_shufflevector(w, w, 4, 5, 6, 7);
   if (l.simple) {
     W += l.first;
     if (MASTER) {
-      float* X = p.master + l.first;
+      float* X = master_of(p) + l.first;
       list_store<4>(X + l.at0, w0);
       list_store<4>(X + l.at1, w1);
     }
@@ -258,19 +274,20 @@ __device__ __forceinline__ void store_q8(const AdamWQ8Tensor& p, const LaneQ8& l
     }
     return;
   }
-  const RowWalk walk(l.first, p.cols);
+  const Lengths len = lengths_of(p);
+  const RowWalk walk(l.first, len.cols);
   const RowWalk::Place p0 = walk.at(l.at0);
   if (ROW && l.n0 >= 8 && p0.left >= 8) {
-    list_store<8>(W + p0.offset(p.ldw), w);
+    list_store<8>(W + p0.offset(len.ldw), w);
     return;
   }
   const RowWalk::Place p1 = walk.at(l.at1);
   if (MASTER) {
-    row_store<4>(p.master, p.cols, p.cols, p0, l.n0, w0);
-    row_store<4>(p.master, p.cols, p.cols, p1, l.n1, w1);
+    row_store<4>(master_of(p), len.cols, len.cols, p0, l.n0, w0);
+    row_store<4>(master_of(p), len.cols, len.cols, p1, l.n1, w1);
   }
-  row_store<4>(W, p.ldw, p.cols, p0, l.n0, w0);
-  row_store<4>(W, p.ldw, p.cols, p1, l.n1, w1);
+  row_store<4>(W, len.ldw, len.cols, p0, l.n0, w0);
+  row_store<4>(W, len.ldw, len.cols, p1, l.n1, w1);
 }
 
 typedef uint32_t q_u32x2 __attribute__((ext_vector_type(2)));
@@ -308,16 +325,16 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const LaneQ8& l, bool ro
   }
 }
 
-__global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const AdamWQ8Group grp) {
+template <class List> __global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const List grp) {
   Scalars s;
   if (!scalars(grp.call, s)) return;
   const int block = grp.call.block0 + span_of_block();
   const int i = tensor_of_block(grp.begin, grp.call.count, block);
-  const AdamWQ8Tensor& p = grp.t[i];
+  const auto& p = grp.t[i];
   s.keep = __builtin_fmaf(-s.lr, p.decay, 1.f);
   const int64_t first = (int64_t)(block - grp.begin[i]) * kSpanQ8, rest = p.count - first;
   const int n = rest < kSpanQ8 ? (int)rest : kSpanQ8;
-  const int types = grp.types[i] + (p.master ? 4 : 0);
+  const int types = grp.types[i] + (master_of(p) ? 4 : 0);
   const int b = threadIdx.x / kLanes, base = b * kBlock, len = n - base;
   if (len <= 0) return;   // the 32 lanes of a block stay together
   // A lane's elements: 4 and the 4 that are 128 further on, so that the 16-byte accesses of fp32 lanes follow each other
@@ -325,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void adamw_q8_list_kernel(const AdamWQ8Gr
   // place in the row instead of two to find where rows lie apart (32.8M elements: 66 us, and 76 with two groups of 4).
   const bool row = types == 3;
   const int lane = threadIdx.x % kLanes, at0 = base + (row ? lane * 8 : lane * 4), at1 = row ? at0 + 4 : at0 + kBlock / 2;
-  const LaneQ8 l{first, at0, at1, n - at0, n - at1, p.ldw == p.cols && p.ldg == p.cols && len >= kBlock};
+  const LaneQ8 l{first, at0, at1, n - at0, n - at1, lengths_of(p).run() && len >= kBlock};
   uint8_t* const Mc = p.Mc + first;
   uint8_t* const Vc = p.Vc + first;
   float* const Ms = p.Ms + (first >> 8);
@@ -364,11 +381,13 @@ __global__ void adamw_tick_kernel(AdamWClock* clock, double beta1, double beta2,
 }
 
 // Spans of the list's tensors and the launches over them: one, unless a launch cannot have so many workgroups.
-template <class Group, class Kernel> hipError_t launch_spans(Group& g, int64_t span, Kernel kernel, hipStream_t stream) {
+template <class Tensor, int N>
+hipError_t launch_spans(AdamWList<Tensor, N>& g, int64_t span, void (*kernel)(AdamWList<Tensor, N>), hipStream_t stream) {
+  if (g.call.count > N) return hipErrorInvalidValue;
   int64_t blocks = 0;
   for (int i = 0; i < g.call.count; ++i) {
     g.begin[i] = (int32_t)blocks;
-    blocks += (g.t[i].count + span - 1) / span;
+    blocks += ((int64_t)g.t[i].count + span - 1) / span;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
   }
   for (int64_t b = 0; b < blocks; b += kMaxBlocks) {
@@ -388,14 +407,9 @@ hipError_t launch_adamw_tick(AdamWClock* clock, float beta1, float beta2, const 
   return hipGetLastError();
 }
 
-hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream) {
-  if (g.call.count > kAdamWTensors) return hipErrorInvalidValue;
-  return launch_spans(g, kSpan, adamw_list_kernel, stream);
-}
-
-hipError_t launch_adamw_q8(AdamWQ8Group& g, hipStream_t stream) {
-  if (g.call.count > kAdamWQ8Tensors) return hipErrorInvalidValue;
-  return launch_spans(g, kSpanQ8, adamw_q8_list_kernel, stream);
-}
+hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream) { return launch_spans(g, kSpan, adamw_list_kernel<AdamWGroup>, stream); }
+hipError_t launch_adamw(AdamWRunGroup& g, hipStream_t stream) { return launch_spans(g, kSpan, adamw_list_kernel<AdamWRunGroup>, stream); }
+hipError_t launch_adamw(AdamWQ8Group& g, hipStream_t stream) { return launch_spans(g, kSpanQ8, adamw_q8_list_kernel<AdamWQ8Group>, stream); }
+hipError_t launch_adamw(AdamWQ8RunGroup& g, hipStream_t stream) { return launch_spans(g, kSpanQ8, adamw_q8_list_kernel<AdamWQ8RunGroup>, stream); }
 
 }  // namespace galore

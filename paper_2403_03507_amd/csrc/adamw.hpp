@@ -21,8 +21,8 @@ struct AdamWClock {
 hipError_t launch_adamw_tick(AdamWClock* clock, float beta1, float beta2, const GradStats* stats, hipStream_t stream);
 
 // A kernel's arguments stay under 4 KiB: so many tensors per launch.
-constexpr int kAdamWTensors = 56;
-constexpr int kAdamWQ8Tensors = 44;
+constexpr int kAdamWTensors = 56, kAdamWRuns = 89;
+constexpr int kAdamWQ8Tensors = 44, kAdamWQ8Runs = 66;
 constexpr int kGradTensors = 128;
 
 struct AdamWTensor {
@@ -49,6 +49,28 @@ struct AdamWQ8Tensor {
   float decay;
 };
 
+// A tensor without a master copy and without gaps between its rows, of fewer than 2^31 elements: what most lists hold.  The
+// shorter description saves launches of long lists (65 norm weights of 4096: one instead of two, 9.2 us a call instead of 11.6;
+// 279 matrices and vectors with 8-bit moments: five instead of seven, 82.6 instead of 92.7).
+struct AdamWRun {
+  void* W;
+  const void* G;
+  float* M;
+  float* V;
+  int32_t count;
+  float decay;
+};
+struct AdamWQ8Run {
+  void* W;
+  const void* G;
+  uint8_t* Mc;
+  uint8_t* Vc;
+  float* Ms;
+  float* Vs;
+  int32_t count;
+  float decay;
+};
+
 struct AdamWCall {
   const GradStats* stats;  // NULL: gradients as they are
   const AdamWClock* clock; // NULL: lr and the corrections below
@@ -65,12 +87,17 @@ template <class Tensor, int N> struct AdamWList {
   Tensor t[N];
 };
 typedef AdamWList<AdamWTensor, kAdamWTensors> AdamWGroup;
+typedef AdamWList<AdamWRun, kAdamWRuns> AdamWRunGroup;
 typedef AdamWList<AdamWQ8Tensor, kAdamWQ8Tensors> AdamWQ8Group;
-static_assert(sizeof(AdamWGroup) <= 4096 && sizeof(AdamWQ8Group) <= 4096, "kernel arguments");
+typedef AdamWList<AdamWQ8Run, kAdamWQ8Runs> AdamWQ8RunGroup;
+static_assert(sizeof(AdamWGroup) <= 4096 && sizeof(AdamWRunGroup) <= 4096, "kernel arguments");
+static_assert(sizeof(AdamWQ8Group) <= 4096 && sizeof(AdamWQ8RunGroup) <= 4096, "kernel arguments");
 
 // The host fills everything but begin and block0.
 hipError_t launch_adamw(AdamWGroup& g, hipStream_t stream);
-hipError_t launch_adamw_q8(AdamWQ8Group& g, hipStream_t stream);
+hipError_t launch_adamw(AdamWRunGroup& g, hipStream_t stream);
+hipError_t launch_adamw(AdamWQ8Group& g, hipStream_t stream);
+hipError_t launch_adamw(AdamWQ8RunGroup& g, hipStream_t stream);
 
 struct GradTensor {
   void* G;

@@ -4,6 +4,7 @@
 #include "api_internal.hpp"
 
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 using namespace galore;
@@ -168,35 +169,49 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
   }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipSuccess;
-  AdamWGroup g{};
-  AdamWQ8Group q{};
-  g.call = q.call = call;
-  const auto types = [&](int32_t i) { return (uint8_t)((W[i].dtype == GALORE_BF16 ? 1 : 0) | (G[i].dtype == GALORE_BF16 ? 2 : 0)); };
-  const auto common = [&](auto& t, int32_t i) {
+  // Tensors of one state format share launches; the short descriptions if they suit all of them.
+  const auto is_q8 = [&](int32_t i) { return S[i].m.dtype == GALORE_U8; };
+  const auto fill = [&](auto& t, int32_t i) {
     t.W = W[i].data; t.G = G[i].data;
-    t.master = static_cast<float*>(S[i].master.data);
-    t.count = W[i].rows * W[i].cols;
-    t.cols = (int32_t)W[i].cols; t.ldw = run_ld(W[i]); t.ldg = run_ld(G[i]);
     t.decay = S[i].weight_decay;
-  };
-  for (int32_t i = 0; i < count && e == hipSuccess; ++i) {
-    if (S[i].m.dtype == GALORE_U8) {
-      const int j = q.call.count++;
-      common(q.t[j], i);
-      q.types[j] = types(i);
-      q.t[j].Mc = static_cast<uint8_t*>(S[i].m.data); q.t[j].Vc = static_cast<uint8_t*>(S[i].v.data);
-      q.t[j].Ms = static_cast<float*>(S[i].m_scale.data); q.t[j].Vs = static_cast<float*>(S[i].v_scale.data);
-      if (q.call.count == kAdamWQ8Tensors) { e = launch_adamw_q8(q, stream); q.call.count = 0; }
-    } else {
-      const int j = g.call.count++;
-      common(g.t[j], i);
-      g.types[j] = types(i);
-      g.t[j].M = static_cast<float*>(S[i].m.data); g.t[j].V = static_cast<float*>(S[i].v.data);
-      if (g.call.count == kAdamWTensors) { e = launch_adamw(g, stream); g.call.count = 0; }
+    if constexpr (std::is_same<decltype(t.count), int64_t>::value) {
+      t.master = static_cast<float*>(S[i].master.data);
+      t.cols = (int32_t)W[i].cols; t.ldw = run_ld(W[i]); t.ldg = run_ld(G[i]);
     }
+    t.count = static_cast<decltype(t.count)>(W[i].rows * W[i].cols);
+  };
+  const auto fill_f32 = [&](auto& t, int32_t i) {
+    fill(t, i);
+    t.M = static_cast<float*>(S[i].m.data); t.V = static_cast<float*>(S[i].v.data);
+  };
+  const auto fill_q8 = [&](auto& t, int32_t i) {
+    fill(t, i);
+    t.Mc = static_cast<uint8_t*>(S[i].m.data); t.Vc = static_cast<uint8_t*>(S[i].v.data);
+    t.Ms = static_cast<float*>(S[i].m_scale.data); t.Vs = static_cast<float*>(S[i].v_scale.data);
+  };
+  const auto launch = [&](auto group, bool q8, const auto& fill_one) -> hipError_t {
+    constexpr int kMost = (int)(sizeof(group.t) / sizeof(group.t[0]));
+    group.call = call;
+    for (int32_t i = 0; i < count; ++i) {
+      if (is_q8(i) != q8) continue;
+      const int j = group.call.count++;
+      group.types[j] = (uint8_t)((W[i].dtype == GALORE_BF16 ? 1 : 0) | (G[i].dtype == GALORE_BF16 ? 2 : 0));
+      fill_one(group.t[j], i);
+      if (group.call.count == kMost) {
+        const hipError_t e = launch_adamw(group, stream);
+        if (e != hipSuccess) return e;
+        group.call.count = 0;
+      }
+    }
+    return launch_adamw(group, stream);
+  };
+  int32_t tensors[2] = {0, 0}, runs[2] = {0, 0};   // by format
+  for (int32_t i = 0; i < count; ++i) {
+    ++tensors[is_q8(i)];
+    runs[is_q8(i)] += !S[i].master.data && run_ld(W[i]) == W[i].cols && run_ld(G[i]) == G[i].cols && W[i].rows * W[i].cols <= INT32_MAX;
   }
-  if (e == hipSuccess) e = launch_adamw(g, stream);
-  if (e == hipSuccess) e = launch_adamw_q8(q, stream);
+  if (tensors[0]) e = runs[0] == tensors[0] ? launch(AdamWRunGroup{}, false, fill_f32) : launch(AdamWGroup{}, false, fill_f32);
+  if (e == hipSuccess && tensors[1]) e = runs[1] == tensors[1] ? launch(AdamWQ8RunGroup{}, true, fill_q8) : launch(AdamWQ8Group{}, true, fill_q8);
   return e == hipSuccess ? GALORE_OK : hip_fail(nullptr, e, "AdamW launch");
 } catch (...) {
   return fail(nullptr, GALORE_ERR_INVALID_ARG, "out of host memory");

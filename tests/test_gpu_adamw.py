@@ -72,18 +72,19 @@ def _within(got, want, bound, dtype=torch.float32):
     assert np.all(ok), (float(err.max()), float((err / np.maximum(bound + STORED[dtype] * np.abs(want), 1e-300)).max()), int((~ok).sum()))
 
 
+@pytest.mark.parametrize("gaps", [True, False])
 @pytest.mark.parametrize("scale", [None, 0.37])
 @pytest.mark.parametrize("wdt,gdt,master", [("f32", "f32", False), ("f32", "bf16", False), ("bf16", "bf16", False), ("bf16", "f32", False),
                                             ("bf16", "bf16", True), ("bf16", "f32", True)])
-def test_one_step_of_a_list_of_all_sizes(wdt, gdt, master, scale):
+def test_one_step_of_a_list_of_all_sizes(wdt, gdt, master, scale, gaps):
     rng = np.random.default_rng(11)
     stats = None if scale is None else _stats(scale)
     s = 1.0 if scale is None else f32(scale)
     W, G, decay, start = [], [], [], []
     for i, shape in enumerate(SIZES):
         pad, off = ((0, 0), (3, 0), (0, 1), (5, 3))[i % 4]
-        W.append(_place(_rand(rng, *shape), TDT[wdt], pad, off))
-        G.append(_place(_rand(rng, *shape), TDT[gdt], (i % 3) * 2, i % 2))
+        W.append(_place(_rand(rng, *shape), TDT[wdt], pad * gaps, off))
+        G.append(_place(_rand(rng, *shape), TDT[gdt], (i % 3) * 2 * gaps, i % 2))
         decay.append(WD if i % 2 else 0.0)
     opt = gb.GaLoreAdamW([w for _, w in W], master=master, beta1=B1, beta2=B2, eps=EPS, weight_decay=decay)
     opt.t = 6
@@ -114,8 +115,8 @@ def test_one_step_of_a_list_of_all_sizes(wdt, gdt, master, scale):
         assert not rest.any()
 
 
-@pytest.mark.parametrize("master", [False, True])
-def test_eight_bit_moments_equal_the_format_bit_for_bit(master):
+@pytest.mark.parametrize("master,gaps", [(False, True), (False, False), (True, True)])
+def test_eight_bit_moments_equal_the_format_bit_for_bit(master, gaps):
     # codes and scales against the checker that replays the fp32 operations of the format; the weight follows from its N
     rng = np.random.default_rng(5)
     sizes = SIZES + [(40, 512), (3, 771), (9, 20000)]
@@ -124,8 +125,8 @@ def test_eight_bit_moments_equal_the_format_bit_for_bit(master):
             continue
         W, G, ref = [], [], []
         for i, shape in enumerate(sizes):
-            W.append(_place(_rand(rng, *shape), TDT[wdt], (i % 3) * 4, i % 2))
-            G.append(_place(_rand(rng, *shape), TDT[gdt], (i % 2) * 3, (i % 4)))
+            W.append(_place(_rand(rng, *shape), TDT[wdt], (i % 3) * 4 * gaps, i % 2))
+            G.append(_place(_rand(rng, *shape), TDT[gdt], (i % 2) * 3 * gaps, (i % 4)))
         opt = gb.GaLoreAdamW([w for _, w in W], moments="q8", master=master, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD)
         for shape in sizes:
             n = shape[0] * shape[1]
@@ -202,9 +203,9 @@ def test_blocks_of_256_are_those_of_the_low_rank_state():
 
 @pytest.mark.parametrize("moments", ["f32", "q8"])
 def test_long_lists_and_splits_of_a_list_give_the_same_bits(moments):
-    # 150 tensors: several launches; the same tensors one call each
+    # 200 tensors: several launches; the same tensors one call each, and those in a list with one that has gaps between rows
     rng = np.random.default_rng(2)
-    shapes = [(1, int(n)) for n in rng.integers(1, 3000, 150)]
+    shapes = [(1, int(n)) for n in rng.integers(1, 3000, 200)]
     W0 = [torch.from_numpy(_rand(rng, *s)).float().cuda() for s in shapes]
     G = [torch.from_numpy(_rand(rng, *s)).bfloat16().cuda() for s in shapes]
     Wa, Wb = [w.clone() for w in W0], [w.clone() for w in W0]
@@ -214,8 +215,13 @@ def test_long_lists_and_splits_of_a_list_give_the_same_bits(moments):
         a.step(Wa, G, 1e-2)
         for o, w, g in zip(singles, Wb, G):
             o.step([w], [g], 1e-2)
+    Wc = [w.clone() for w in W0] + [torch.zeros(5, 9, device="cuda")[:, :7]]
+    c = gb.GaLoreAdamW(Wc, moments=moments, weight_decay=0.1)
+    for _ in range(2):
+        c.step(Wc, G + [torch.ones(5, 7, device="cuda")], 1e-2)
     for i, o in enumerate(singles):
         assert torch.equal(Wa[i], Wb[i]) and torch.equal(a.M[i], o.M[0]) and torch.equal(a.V[i], o.V[0]), i
+        assert torch.equal(Wa[i], Wc[i]) and torch.equal(a.M[i], c.M[i]) and torch.equal(a.V[i], c.V[i]), i
 
 
 def test_both_state_formats_and_both_types_in_one_call():
