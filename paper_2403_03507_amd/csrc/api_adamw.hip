@@ -98,7 +98,7 @@ int32_t run_ld(const galore_tensor& t) { return (int32_t)(t.rows == 1 ? t.cols :
 galore_status fill_grads(const galore_tensor* G, int32_t count, std::vector<GradGroup>& lists) {
   if (count < 0) return fail(nullptr, GALORE_ERR_INVALID_ARG, "count %d < 0", count);
   if (count > 0 && !G) return fail(nullptr, GALORE_ERR_INVALID_ARG, "G is NULL");
-  lists.resize((size_t)(count + kGradTensors - 1) / kGradTensors);
+  lists.resize(((size_t)count + kGradTensors - 1) / kGradTensors);
   for (int32_t i = 0; i < count; ++i) {
     galore_status s = check_matrix(nullptr, G[i], "G", i, true);
     if (s || (s = check_element_alignment(G[i], "G", i))) return s;
@@ -136,7 +136,7 @@ galore_status galore_adamw(const galore_tensor* W, const galore_tensor* G, const
         (s = check_element_alignment(W[i], "W", i)) || (s = check_element_alignment(G[i], "G", i)))
       return s;
     if (G[i].rows != W[i].rows || G[i].cols != W[i].cols) return fail(nullptr, GALORE_ERR_SHAPE, "G[%d] must have W's shape", i);
-    if (!(st.weight_decay >= 0.f)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "weight_decay of tensor %d out of range", i);
+    if (!(st.weight_decay >= 0.f) || !std::isfinite(st.weight_decay)) return fail(nullptr, GALORE_ERR_INVALID_ARG, "weight_decay of tensor %d out of range", i);
     const bool q8 = st.m.dtype == GALORE_U8;
     if ((s = check_moment(st.m, "m", i, W[i], q8 ? GALORE_U8 : GALORE_F32)) || (s = check_moment(st.v, "v", i, W[i], q8 ? GALORE_U8 : GALORE_F32)))
       return s;

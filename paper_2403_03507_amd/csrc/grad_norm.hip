@@ -82,7 +82,12 @@ template <bool CACHED> __global__ __launch_bounds__(kNormThreads) void grad_squa
 
 __global__ __launch_bounds__(kNormThreads) void grad_stats_kernel(const double* partials, int count, float grad_scale, float max_norm, GradStats* stats) {
   double x = 0.0;
-  for (int i = threadIdx.x; i < count; i += kNormThreads) x += partials[i];
+  for (int base = threadIdx.x; base < count; base += 4 * kNormThreads) {   // four requests at a time
+    double y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = base + j * kNormThreads < count ? partials[base + j * kNormThreads] : 0.0;
+    x += (y[0] + y[1]) + (y[2] + y[3]);
+  }
   x = workgroup_sum(x);
   if (threadIdx.x == 0) {
     const bool finite = x <= 1.7976931348623157e308;   // false for NaN

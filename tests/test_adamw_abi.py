@@ -46,8 +46,9 @@ def test_adamw_refuses_bad_scalars():
     assert c.status() == 1
     c = Call(); c.S[1].weight_decay = -1.0
     assert c.status() == 1
-    c = Call(); c.S[1].weight_decay = float("nan")
-    assert c.status() == 1
+    for bad in (float("nan"), float("inf")):
+        c = Call(); c.S[1].weight_decay = bad
+        assert c.status() == 1
     c = Call(); c.stats = BASE + 4
     assert c.status() == 5
     c = Call(); c.clock = BASE + 4
