@@ -117,7 +117,7 @@ def test_one_step_of_a_list_of_all_sizes(wdt, gdt, master, scale, gaps):
 
 @pytest.mark.parametrize("master,gaps", [(False, True), (False, False), (True, True)])
 def test_eight_bit_moments_equal_the_format_bit_for_bit(master, gaps):
-    # codes and scales against the checker that replays the fp32 operations of the format; the weight follows from its N
+    # codes and scales against the oracle that replays the fp32 operations of the format; the weight follows from its N
     rng = np.random.default_rng(5)
     sizes = SIZES + [(40, 512), (3, 771), (9, 20000)]
     for wdt, gdt in (("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")):
@@ -149,7 +149,7 @@ def test_eight_bit_moments_equal_the_format_bit_for_bit(master, gaps):
                 assert np.array_equal(np.where(got == 0x80, 0, got), np.where(Mc == 0x80, 0, Mc)), (i, k)   # the zero's sign is free
                 assert np.array_equal(opt.V[i].cpu().numpy().reshape(-1), Vc), (i, k)
                 assert np.array_equal(opt.M_scale[i].cpu().numpy(), Ms) and np.array_equal(opt.V_scale[i].cpu().numpy(), Vs), (i, k)
-                # n once more with other roundings.  The checker rounds m c1, the square root, the sum and the quotient (u
+                # n once more with other roundings.  The oracle rounds m c1, the square root, the sum and the quotient (u
                 # each); the kernel's square root and reciprocal are good to one unit in the last place (2u each), and it
                 # rounds lr c1, the sum and m times the reciprocal: 4u + 4u + 3u = 11u of n
                 want = (1 - LR * WD) * before[i] - LR * n
