@@ -442,8 +442,12 @@ galore_status galore_adamw_tick(galore_adamw_clock* clock, float beta1, float be
  * in fp32, W rounded once.  With a clock (else NULL), lr and k are those on the device and the arguments are not used.
  * If stats->finite is not 1 the call leaves every tensor as it was (a k of the caller's should then be used once more).
  * Without stats, entries of G that are not finite make their weight and moments (8-bit moments: their block) non-finite.
- * The second moment is formed in fp32: entries of g beyond about 1e19 in magnitude overflow it (their weight then only
- * decays), as squares below 1e-38 vanish in it.  (With 8-bit moments v / (1-beta2^k) counts as 1.2e-38 where it is less.)
+ * The second moment is formed in fp32: entries of g beyond about 1e19 in magnitude overflow it, as squares below 1e-38
+ * vanish in it.  The weight of an entry that overflows it only decays, from that step on.  With 8-bit moments it also makes
+ * its block's v_scale infinite, and the block's 256 weights (masters) and v_scale are NaN from the next step on: neither
+ * an overflowed second moment nor one that was loaded so gives finite weights.  (galore_grad_norm's finite is 1 for such
+ * entries; its factor, with a finite max_norm, keeps g below them.  With 8-bit moments v / (1-beta2^k) counts as 1.2e-38
+ * where it is less.)
  * One launch for up to 89 tensors with fp32 moments, and one for up to 66 with 8-bit ones (56 and 44 if one of them has a
  * master copy, gaps between rows of W or G, or 2^31 elements).
  * GALORE_ERR_INVALID_ARG if two of the written tensors (W, m, v, scales, master) start at the same address, or a gradient

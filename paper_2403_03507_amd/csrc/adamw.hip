@@ -190,8 +190,9 @@ __device__ __forceinline__ void step_q8(const ListF32<8>& g, ListF32<8>& w, uint
     float gv = omb2 * ge;
     gv = gv * ge;
     v[e] = __builtin_fmaf(s.beta2, v[e], gv);
-    // the approximations take no subnormal numbers: 1.1e-19 is the smallest square root (and 0 / 0 at eps = 0 is 0)
-    const float den = __builtin_amdgcn_sqrtf(fmaxf(v[e] * s.inv_c2, 0x1p-126f)) + s.eps;
+    // the approximations take no subnormal numbers: 1.1e-19 is the smallest square root (and 0 / 0 at eps = 0 is 0).  The
+    // maximum keeps NaN: a block whose scale overflowed decodes to it, and a number in its place would be a step of m / eps
+    const float den = __builtin_amdgcn_sqrtf(__builtin_elementwise_maximum(v[e] * s.inv_c2, 0x1p-126f)) + s.eps;
     w[e] = __builtin_fmaf(rate, m[e] * __builtin_amdgcn_rcpf(den), s.keep * w[e]);
     amax = __builtin_elementwise_maximum(amax, __builtin_fabsf(m[e]));
     vmax = __builtin_elementwise_maximum(vmax, v[e]);
