@@ -75,15 +75,19 @@ class PerLayerGaLore:
     def finish(self, stats=None):
         """Call after backward(): steps the other parameters and drops their gradients, and orders the library's
         streams before torch's current stream.  stats: what a `binding.GaLoreGradNorm` measured of the other
-        parameters' gradients (those of the GaLore matrices are gone by now)."""
-        if self.others:
-            grads = [p.grad for p in self.others]
-            if any(g is None for g in grads):
-                raise ValueError("a parameter of `others` has no gradient")
-            self.others_opt.step(self._others_array, grads, self.others_lr, stats)
-            for p in self.others:
-                p.grad = None
-        self.opt.join()
+        parameters' gradients (those of the GaLore matrices are gone by now).  Every parameter of `others` needs a
+        gradient: without one ValueError is raised and none of them is stepped.  The streams are ordered also where
+        this raises, and the gradients of `others` are kept then."""
+        try:
+            if self.others:
+                grads = [p.grad for p in self.others]
+                if any(g is None for g in grads):
+                    raise ValueError("a parameter of `others` has no gradient")
+                self.others_opt.step(self._others_array, grads, self.others_lr, stats)
+                for p in self.others:
+                    p.grad = None
+        finally:
+            self.opt.join()
 
     def close(self):
         for h in self._handles:

@@ -1,0 +1,62 @@
+"""What the Python face of AdamW over tensor lists does on the host: order of calls, refusals (no GPU)."""
+import pytest
+import torch
+
+from paper_2403_03507_amd import binding as gb
+from paper_2403_03507_amd.hooks import PerLayerGaLore
+
+
+class _Recorder:
+    """Stands in for the library's two optimizers of a PerLayerGaLore and notes the calls."""
+
+    def __init__(self, error=None):
+        self.calls, self.error = [], error
+
+    def join(self):
+        self.calls.append("join")
+
+    def step(self, weights, grads, lr, stats=None):
+        self.calls.append("step")
+        if self.error:
+            raise self.error
+
+
+def _driver(others, error=None):
+    drv = object.__new__(PerLayerGaLore)
+    drv.opt = drv.others_opt = _Recorder(error)
+    drv.others, drv.others_lr, drv._others_array = others, 1e-3, None
+    return drv
+
+
+def _params(n):
+    params = [torch.nn.Parameter(torch.ones(3)) for _ in range(n)]
+    for p in params:
+        p.grad = torch.ones(3)
+    return params
+
+
+def test_finish_joins_the_streams_when_it_raises():
+    # the hooks have started GaLore steps on the library's streams: whatever finish() refuses, they are ordered first
+    params = _params(3)
+    params[1].grad = None
+    drv = _driver(params)
+    with pytest.raises(ValueError):
+        drv.finish()
+    assert drv.opt.calls == ["join"]                                             # and nothing was stepped
+    assert params[0].grad is not None and params[2].grad is not None
+    for error in (ValueError("a gradient of another kind"), gb.GaloreError(1, "refused")):
+        params = _params(2)
+        drv = _driver(params, error)
+        with pytest.raises(type(error)):
+            drv.finish()
+        assert drv.opt.calls == ["step", "join"] and all(p.grad is not None for p in params)
+
+
+def test_finish_steps_and_joins():
+    params = _params(2)
+    drv = _driver(params)
+    drv.finish()
+    assert drv.opt.calls == ["step", "join"] and all(p.grad is None for p in params)
+    drv = _driver([])
+    drv.finish()
+    assert drv.opt.calls == ["join"]
