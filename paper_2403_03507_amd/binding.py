@@ -6,6 +6,7 @@ if the library is missing this module raises.
 """
 import ctypes
 import functools
+import math
 import os
 
 import torch  # also loads the HIP runtime the library binds to
@@ -544,7 +545,12 @@ class GaLoreAdamW:
         return [x if has else None for x, has in zip(views, self._has_master)]
 
     def set_lr(self, lr):
-        """capturable: the learning rate of the steps from here on (ordered by the current stream)."""
+        """capturable: the learning rate of the steps from here on (ordered by the current stream): a finite number, or a
+        tensor of one element, which is taken as it is."""
+        if self.clock is None:
+            raise ValueError("set_lr() needs capturable=True; else the rate is an argument of step()")
+        if not isinstance(lr, torch.Tensor) and not math.isfinite(lr):
+            raise ValueError("lr is not finite")
         self.clock[8:12].view(torch.float32).fill_(lr)
 
     def count(self):
@@ -552,16 +558,19 @@ class GaLoreAdamW:
         return self.t if self.clock is None else int(self.clock[:8].view(torch.int64))
 
     def step(self, weights, grads, lr=None, stats=None):
-        """weights, grads: tensors in the constructor's order, or arrays of their descriptors.  lr: with capturable=True
-        None, or set_lr() first.  stats: the result of a GaLoreGradNorm; its factor is applied to the gradients, and where
-        an entry was not finite nothing changes (without capturable the step is counted all the same: set `t` back to
-        repeat it)."""
+        """weights, grads: tensors in the constructor's order, or arrays of their descriptors.  lr: the learning rate; with
+        capturable=True None takes the one that set_lr() left, and a number goes through set_lr() here (captured with the
+        step, it is the rate of every replay).  stats: the result of a GaLoreGradNorm; its factor is applied to the
+        gradients, and where an entry was not finite nothing changes.  Such a step counts all the same without capturable,
+        since the host does not wait for the device to say so: a caller that reads `finite` sets `t` back by one."""
         if self.clock is not None:
             if lr is not None:
                 self.set_lr(lr)
             galore_adamw_tick(self.clock, self.beta1, self.beta2, stats)
             galore_adamw(weights, grads, self._states, self.beta1, self.beta2, self.eps, 0.0, 1, stats, self.clock)
             return
+        if lr is None:
+            raise ValueError("step() needs lr without capturable=True")
         galore_adamw(weights, grads, self._states, self.beta1, self.beta2, self.eps, lr, self.t + 1, stats)
         self.t += 1
 

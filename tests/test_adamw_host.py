@@ -60,3 +60,22 @@ def test_finish_steps_and_joins():
     drv = _driver([])
     drv.finish()
     assert drv.opt.calls == ["join"]
+
+
+def test_rates_that_no_step_could_take_are_refused():
+    plain, captured = gb.GaLoreAdamW([], device="cpu"), gb.GaLoreAdamW([], device="cpu", capturable=True)
+    with pytest.raises(ValueError):
+        plain.set_lr(1e-3)                                                       # has no rate on the device
+    with pytest.raises(ValueError):
+        plain.step([], [])                                                       # nor one of its own
+    assert plain.t == 0
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        with pytest.raises(ValueError):
+            captured.set_lr(bad)
+        with pytest.raises(ValueError):
+            captured.step([], [], bad)
+        assert not captured.clock.any()
+    captured.set_lr(0.25)
+    assert float(captured.clock[8:12].view(torch.float32)) == 0.25
+    captured.set_lr(torch.tensor(0.5))                                           # a schedule's tensor is not looked at
+    assert float(captured.clock[8:12].view(torch.float32)) == 0.5
