@@ -434,6 +434,8 @@ def galore_grad_norm_workspace_bytes(count):
 
 def galore_grad_norm(G, grad_scale, max_norm, stats, workspace):
     G = _param_array(G)
+    if workspace.get_device() != torch._C._cuda_getDevice() or workspace.dtype != torch.uint8 or workspace.dim() != 1 or workspace.stride(0) != 1:
+        raise ValueError("workspace: contiguous bytes on the current device")
     _check(lib().galore_grad_norm(G, len(G), grad_scale, max_norm, _stats_ptr(stats), workspace.data_ptr(), workspace.numel(), _stream()))
 
 
@@ -488,6 +490,8 @@ class GaLoreAdamW:
         if len(decay) != len(weights):
             raise ValueError("one weight_decay per tensor")
         descs = [param_desc(w) for w in weights]  # refuses what a step could not take
+        if weights and torch.empty(0, device=device).device != weights[0].device:
+            raise ValueError("device: the states belong on the weights' device")
         starts, total = [], 0
         for d in descs:
             starts.append(total)
@@ -563,6 +567,8 @@ class GaLoreAdamW:
         step, it is the rate of every replay).  stats: the result of a GaLoreGradNorm; its factor is applied to the
         gradients, and where an entry was not finite nothing changes.  Such a step counts all the same without capturable,
         since the host does not wait for the device to say so: a caller that reads `finite` sets `t` back by one."""
+        if self._places and self.M_flat.get_device() != torch._C._cuda_getDevice():
+            raise ValueError("the states are on another device than the current one")
         if self.clock is not None:
             if lr is not None:
                 self.set_lr(lr)

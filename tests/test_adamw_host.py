@@ -79,3 +79,41 @@ def test_rates_that_no_step_could_take_are_refused():
     assert float(captured.clock[8:12].view(torch.float32)) == 0.25
     captured.set_lr(torch.tensor(0.5))                                           # a schedule's tensor is not looked at
     assert float(captured.clock[8:12].view(torch.float32)) == 0.5
+
+
+def _described(monkeypatch):
+    """param_desc of host tensors as if they were the device's: only what happens before a launch is looked at."""
+    monkeypatch.setattr(gb, "param_desc", lambda t: gb.galore_tensor(1 << 20, 1, t.numel(), t.numel(), gb.GALORE_F32))
+
+
+def test_states_on_another_device_than_the_weights_are_refused(monkeypatch):
+    _described(monkeypatch)
+    w = torch.zeros(8)
+    for options in ({}, {"moments": "q8"}, {"capturable": True}):
+        with pytest.raises(ValueError, match="device"):
+            gb.GaLoreAdamW([w], device="meta", **options)
+    assert gb.GaLoreAdamW([w], device="cpu").M_flat.device == w.device
+
+
+def test_a_step_on_another_device_than_the_states_is_refused(monkeypatch):
+    _described(monkeypatch)
+    calls = []
+    monkeypatch.setattr(gb, "galore_adamw", lambda *a: calls.append(a))
+    opt = gb.GaLoreAdamW([torch.zeros(8)], device="cpu")                         # where get_device() is -1
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    array = gb.tensor_array([gb.galore_tensor(1 << 20, 1, 8, 8, gb.GALORE_F32)])
+    with pytest.raises(ValueError, match="device"):
+        opt.step(array, array, 1e-3)
+    assert not calls and opt.t == 0
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    opt.step(array, array, 1e-3)
+    assert len(calls) == 1 and opt.t == 1
+
+
+def test_a_workspace_that_is_no_device_memory_is_refused(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(gb, "_stats_ptr", lambda stats: 1 << 20)
+    need = gb.galore_grad_norm_workspace_bytes(1)
+    array = gb.tensor_array([gb.galore_tensor(1 << 20, 1, 8, 8, gb.GALORE_F32)])
+    with pytest.raises(ValueError, match="workspace"):
+        gb.galore_grad_norm(array, 1.0, 1.0, None, torch.zeros(need, dtype=torch.uint8))
