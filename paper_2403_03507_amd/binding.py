@@ -500,9 +500,9 @@ class GaLoreAdamW:
         self._has_master = [master and d.dtype == GALORE_BF16 for d in descs]
         q8 = moments == "q8"
         code, dt, size = (torch.uint8, GALORE_U8, 1) if q8 else (torch.float32, GALORE_F32, 4)
-        self.M_flat, self.V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
-        self.M_scale_flat, self.V_scale_flat = ((torch.zeros(total // self._ALIGN, device=device) for _ in range(2)) if q8 else (None, None))
-        self.master_flat = torch.zeros(total, device=device) if master else None
+        self._M_flat, self._V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
+        self._M_scale_flat, self._V_scale_flat = ((torch.zeros(total // self._ALIGN, device=device) for _ in range(2)) if q8 else (None, None))
+        self._master_flat = torch.zeros(total, device=device) if master else None
         for i, w in enumerate(weights):
             if self._has_master[i]:
                 self.master[i].copy_(w.detach())
@@ -519,8 +519,16 @@ class GaLoreAdamW:
             st.master = at(x, 4, GALORE_F32) if has_master else none
         self.clock = torch.zeros(ctypes.sizeof(galore_adamw_clock), dtype=torch.uint8, device=device) if capturable else None
 
-    # The state of every tensor, as views of the flat buffers (which are what a checkpoint saves, with the step count).
-    # After a weight was replaced (loaded) the caller copies it to its master as well.
+    # The flat buffers are what a checkpoint saves, with the step count (the clock's bytes with capturable), and what a loaded
+    # one is copied into: the states hold their addresses, so none of them can be replaced.
+    M_flat = property(lambda self: self._M_flat)
+    V_flat = property(lambda self: self._V_flat)
+    M_scale_flat = property(lambda self: self._M_scale_flat)
+    V_scale_flat = property(lambda self: self._V_scale_flat)
+    master_flat = property(lambda self: self._master_flat)
+
+    # The state of every tensor, as views of the flat buffers.  After a weight was replaced (loaded) the caller copies it to
+    # its master as well.
     def _views(self, flat):
         return [flat[s:s + n].view(shape) for s, shape, n in self._places]
 

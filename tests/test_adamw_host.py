@@ -117,3 +117,17 @@ def test_a_workspace_that_is_no_device_memory_is_refused(monkeypatch):
     array = gb.tensor_array([gb.galore_tensor(1 << 20, 1, 8, 8, gb.GALORE_F32)])
     with pytest.raises(ValueError, match="workspace"):
         gb.galore_grad_norm(array, 1.0, 1.0, None, torch.zeros(need, dtype=torch.uint8))
+
+
+def test_buffers_whose_addresses_the_states_hold_cannot_be_replaced(monkeypatch):
+    # a loaded state is copied into them: an assignment would leave the library with the address of freed memory
+    _described(monkeypatch)
+    opt = gb.GaLoreAdamW([torch.zeros(8), torch.zeros(300)], moments="q8", device="cpu", capturable=True)
+    for name in ("M_flat", "V_flat", "M_scale_flat", "V_scale_flat", "master_flat"):
+        before = getattr(opt, name)
+        with pytest.raises(AttributeError):
+            setattr(opt, name, torch.zeros(1024, dtype=torch.uint8))
+        assert getattr(opt, name) is before
+    assert opt.M_flat.shape == (768,) and opt.M_scale_flat.shape == (3,) and opt.master_flat is None
+    opt.M_flat.copy_(torch.full((768,), 7, dtype=torch.uint8))                   # tensors start at multiples of 256
+    assert opt.M[1].shape == (300,) and bool((opt.M[1] == 7).all())
