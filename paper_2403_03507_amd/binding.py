@@ -501,8 +501,9 @@ class GaLoreAdamW:
         q8 = moments == "q8"
         code, dt, size = (torch.uint8, GALORE_U8, 1) if q8 else (torch.float32, GALORE_F32, 4)
         self._M_flat, self._V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
-        self._M_scale_flat, self._V_scale_flat = ((torch.zeros(total // self._ALIGN, device=device) for _ in range(2)) if q8 else (None, None))
-        self._master_flat = torch.zeros(total, device=device) if master else None
+        scales = lambda: torch.zeros(total // self._ALIGN, dtype=torch.float32, device=device) if q8 else None
+        self._M_scale_flat, self._V_scale_flat = scales(), scales()
+        self._master_flat = torch.zeros(total, dtype=torch.float32, device=device) if master else None
         for i, w in enumerate(weights):
             if self._has_master[i]:
                 self.master[i].copy_(w.detach())

@@ -131,3 +131,20 @@ def test_buffers_whose_addresses_the_states_hold_cannot_be_replaced(monkeypatch)
     assert opt.M_flat.shape == (768,) and opt.M_scale_flat.shape == (3,) and opt.master_flat is None
     opt.M_flat.copy_(torch.full((768,), 7, dtype=torch.uint8))                   # tensors start at multiples of 256
     assert opt.M[1].shape == (300,) and bool((opt.M[1] == 7).all())
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_states_do_not_follow_the_default_dtype(default, monkeypatch):
+    # the library is told fp32: buffers of the default type would be too short
+    monkeypatch.setattr(gb, "param_desc", lambda t: gb.galore_tensor(1 << 20, 1, t.numel(), t.numel(), gb.GALORE_BF16))
+    w = torch.zeros(300, dtype=torch.bfloat16)
+    torch.set_default_dtype(default)
+    try:
+        q8 = gb.GaLoreAdamW([w], moments="q8", master=True, device="cpu", capturable=True)
+        plain = gb.GaLoreAdamW([w], master=True, device="cpu")
+        norm = gb.GaLoreGradNorm(1, device="cpu")
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert q8.M_scale_flat.dtype == q8.V_scale_flat.dtype == q8.master_flat.dtype == torch.float32
+    assert plain.M_flat.dtype == plain.V_flat.dtype == plain.master_flat.dtype == norm.stats.dtype == torch.float32
+    assert q8.M_flat.dtype == q8.V_flat.dtype == q8.clock.dtype == norm.workspace.dtype == torch.uint8
