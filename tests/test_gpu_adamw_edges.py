@@ -1,4 +1,5 @@
-"""AdamW over tensor lists, gradient norm and scaling on the GPU at their edges: second moments beyond fp32.
+"""AdamW over tensor lists, gradient norm and scaling on the GPU at their edges: second moments beyond fp32, memory next to
+the tensors, ends around a workgroup's elements.
 
 Tolerances count roundings (u = 2^-24, half a step of fp32; 2^-8 for a weight stored in bf16).  W = (1 - lr wd) W - lr n: the
 factor of W, its product and the sum are 2u |W| + u |W'|.  n differs from the oracle's by 11u |n| (the oracle rounds m c1, the
@@ -104,3 +105,68 @@ def test_fp32_second_moment_that_overflows(size):
         same = torch.ones(2100, dtype=torch.bool, device="cuda")
         same[300] = False
         assert torch.equal(w.view(-1)[same], clean.view(-1)[same])
+
+
+# ---- memory next to the tensors --------------------------------------------------------------------
+
+# ends around 8 elements, a block of 256, and what a workgroup takes (512 elements; with 8-bit moments 1024)
+SIZES = [(1, 1), (1, 7), (5, 1), (1, 9), (3, 85), (1, 255), (1, 257), (1, 511), (1, 512), (1, 513), (1, 1023), (1, 1024), (1, 1025),
+         (7, 73), (2, 511), (3, 513), (2, 1023), (33, 31), (9, 1025), (1, 2047), (5, 2049)]
+
+
+def _placed(rng, shape, dtype, gap, offset):
+    """A matrix in a buffer that holds numbers everywhere: none of them may change but the matrix's own."""
+    rows, cols = shape
+    buf = torch.from_numpy(rng.uniform(0.5, 2.0, offset + rows * (cols + gap) + 40) * rng.choice([-1.0, 1.0])).to(TDT[dtype]).cuda()
+    return buf, buf[offset:offset + rows * (cols + gap)].view(rows, cols + gap)[:, :cols]
+
+
+def _around(buf, view):
+    """The buffer with the view's own elements out of it."""
+    inside = torch.zeros(buf.numel(), dtype=torch.bool, device="cuda")
+    inside.as_strided(view.shape, view.stride(), view.storage_offset())[:] = True
+    return buf[~inside]
+
+
+@pytest.mark.parametrize("gaps", [True, False])
+@pytest.mark.parametrize("moments", ["f32", "q8"])
+@pytest.mark.parametrize("wdt,gdt,master", [("f32", "f32", False), ("f32", "bf16", False), ("bf16", "bf16", False), ("bf16", "f32", False),
+                                            ("bf16", "bf16", True), ("bf16", "f32", True)])
+def test_a_step_changes_nothing_next_to_its_tensors(wdt, gdt, master, moments, gaps):
+    rng = np.random.default_rng(31)
+    W = [_placed(rng, s, wdt, gaps * (i % 4) * 3, (0, 1, 3)[i % 3]) for i, s in enumerate(SIZES)]
+    G = [_placed(rng, s, gdt, gaps * (i % 3), i % 2) for i, s in enumerate(SIZES)]
+    weights, grads = [w for _, w in W], [g for _, g in G]
+    opt = gb.GaLoreAdamW(weights, moments=moments, master=master, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD)
+    states = [opt.M_flat, opt.V_flat] + ([opt.master_flat] if master else [])
+    own = torch.zeros(opt.M_flat.numel(), dtype=torch.bool, device="cuda")
+    for m in opt.M:
+        own[m.storage_offset():m.storage_offset() + m.numel()] = True
+    for s in states:
+        s[~own] = 77                                                             # between two tensors' states
+    keep_w, keep_g, before = [_around(*w).clone() for w in W], [b.clone() for b, _ in G], [w.clone() for w in weights]
+    for _ in range(2):
+        opt.step(weights, grads, LR)
+    for i in range(len(SIZES)):
+        assert torch.equal(_around(*W[i]), keep_w[i]), SIZES[i]
+        assert torch.equal(G[i][0], keep_g[i]), SIZES[i]
+        # and every element of its own was stepped: by about lr twice, which bf16 may round away
+        if wdt == "f32":
+            assert bool((weights[i] != before[i]).all()), SIZES[i]
+        assert bool((opt.M[i] != 0).all()), SIZES[i]
+    for s in states:
+        assert bool((s[~own] == 77).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("finite", [1.0, 0.0])
+def test_scaling_changes_nothing_next_to_its_tensors(dtype, finite):
+    rng = np.random.default_rng(32)
+    sizes = SIZES + [(3, 5000), (700, 9), (1, 4096), (1, 4097)]
+    G = [_placed(rng, s, dtype, (i % 4) * 3, (0, 1, 3)[i % 3]) for i, s in enumerate(sizes)]
+    keep, before = [_around(*g).clone() for g in G], [g.clone() for _, g in G]
+    norm = gb.GaLoreGradNorm(len(G))
+    norm.scale([g for _, g in G], torch.tensor([1.0, 0.5 * finite, finite, 0.0], device="cuda"))
+    for i, (buf, view) in enumerate(G):
+        assert torch.equal(_around(buf, view), keep[i]), sizes[i]
+        assert torch.equal(view, before[i] * 0.5 if finite else torch.zeros_like(view)), sizes[i]     # halves are exact
