@@ -1,5 +1,5 @@
 """AdamW over tensor lists, gradient norm and scaling on the GPU at their edges: second moments beyond fp32, memory next to
-the tensors, ends around a workgroup's elements.
+the tensors, ends around a workgroup's elements, lists of many workgroups.
 
 Tolerances count roundings (u = 2^-24, half a step of fp32; 2^-8 for a weight stored in bf16).  W = (1 - lr wd) W - lr n: the
 factor of W, its product and the sum are 2u |W| + u |W'|.  n differs from the oracle's by 11u |n| (the oracle rounds m c1, the
@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from helpers import TDT, f32, to64
+from oracle import adamw_oracle as ao
 from oracle import q8_oracle as q8
 from paper_2403_03507_amd import binding as gb
 
@@ -170,3 +171,54 @@ def test_scaling_changes_nothing_next_to_its_tensors(dtype, finite):
     for i, (buf, view) in enumerate(G):
         assert torch.equal(_around(buf, view), keep[i]), sizes[i]
         assert torch.equal(view, before[i] * 0.5 if finite else torch.zeros_like(view)), sizes[i]     # halves are exact
+
+
+# ---- lists of many workgroups ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("moments,wdt", [("f32", "f32"), ("f32", "bf16"), ("q8", "bf16"), ("q8", "f32")])
+@pytest.mark.parametrize("gap", [0, 3])
+def test_every_element_of_a_list_of_many_workgroups(moments, wdt, gap):
+    # From 4096 workgroups (2.1M elements, with 8-bit moments 4.2M) on a launch numbers them by XCD.  All elements of two full
+    # groups and a rest of such workgroups, against calls on pieces that are too short for that (multiples of 256 elements).
+    rng = np.random.default_rng(33)
+    shapes = [(1, 2500001), (1, 33), (700, 2001), (1, 4100000), (1100, 1101)]
+    total = sum(m * n for m, n in shapes)
+    assert 2 * 4096 * 512 < total and 2 * 4096 * 1024 < total < 3 * 4096 * 1024
+    gen = torch.Generator("cuda").manual_seed(4)
+    rand = lambda m, n: torch.randn(m, n + gap, generator=gen, device="cuda").to(TDT[wdt])[:, :n]
+    W, G = [rand(*s) for s in shapes], [rand(*s) for s in shapes]
+    pieces_w, pieces_g, at = [], [], []
+    for i, (w, g) in enumerate(zip(W, G)):
+        flat_w, flat_g = w.reshape(-1).clone(), g.reshape(-1).clone()
+        for a in range(0, flat_w.numel(), 1 << 20):
+            pieces_w.append(flat_w[a:a + (1 << 20)])
+            pieces_g.append(flat_g[a:a + (1 << 20)])
+            at.append((i, a))
+    opt = gb.GaLoreAdamW(W, moments=moments, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD)
+    singles = [gb.GaLoreAdamW([w], moments=moments, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD) for w in pieces_w]
+    start = [to64(w) for w in W]
+    for _ in range(2):
+        opt.step(W, G, LR)
+        for o, w, g in zip(singles, pieces_w, pieces_g):
+            o.step([w], [g], LR)
+    for (i, a), o, w in zip(at, singles, pieces_w):
+        cut = lambda t: t.reshape(-1)[a:a + w.numel()]
+        assert torch.equal(cut(W[i]), w) and torch.equal(cut(opt.M[i]), o.M[0]) and torch.equal(cut(opt.V[i]), o.V[0]), (i, a)
+        if moments == "q8":
+            blocks = slice(a // 256, a // 256 + o.M_scale[0].numel())
+            assert torch.equal(opt.M_scale[i][blocks], o.M_scale[0]) and torch.equal(opt.V_scale[i][blocks], o.V_scale[0]), (i, a)
+    if moments == "f32":
+        # Both ways could be wrong together: the weights against the oracle.  With one gradient in both steps every sum has terms of
+        # one sign: m is off by 2u, v by 3u; the corrections and their products are 2u each, so that sqrt(v c2) + eps is off by
+        # 5u / 2 + 2u and n by 2u + 2u + 4.5u + u < 10u; the weight's factor, its product and the sum are 3u of it.  The 20u
+        # below leave room for |W'| <= |W| + lr.
+        for i, g in enumerate(G):
+            m, v, w = 0.0, 0.0, start[i]
+            for k in (1, 2):
+                before = w
+                w, m, v, n = ao.adamw(w, to64(g), m, v, B1, B2, EPS, LR, WD, k)
+            largest = np.maximum(np.abs(start[i]), np.abs(before))
+            bound = 2 * (3 * U * largest + LR * 20 * U * np.abs(n) + TINY)
+            if wdt == "bf16":
+                bound = bound + 2 * 2.0 ** -8 * (np.maximum(largest, np.abs(w)) + LR) * 1.01
+            assert np.all(np.abs(to64(W[i]) - w) <= bound)
