@@ -1,5 +1,5 @@
 """AdamW over tensor lists, gradient norm and scaling on the GPU at their edges: second moments beyond fp32, memory next to
-the tensors, ends around a workgroup's elements, lists of many workgroups.
+the tensors, ends around a workgroup's elements, lists of many workgroups, the stream that the calls go to.
 
 Tolerances count roundings (u = 2^-24, half a step of fp32; 2^-8 for a weight stored in bf16).  W = (1 - lr wd) W - lr n: the
 factor of W, its product and the sum are 2u |W| + u |W'|.  n differs from the oracle's by 11u |n| (the oracle rounds m c1, the
@@ -222,3 +222,52 @@ def test_every_element_of_a_list_of_many_workgroups(moments, wdt, gap):
             if wdt == "bf16":
                 bound = bound + 2 * 2.0 ** -8 * (np.maximum(largest, np.abs(w)) + LR) * 1.01
             assert np.all(np.abs(to64(W[i]) - w) <= bound)
+
+
+# ---- the stream ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("call", ["measure", "scale", "step_f32", "step_q8", "tick"])
+def test_a_call_waits_for_its_own_stream(call):
+    # what it reads is written at the end of long work on a stream of the caller's: a call on any other stream would read
+    # what was there before.  All results are exact: powers of two.
+    n = 1 << 20
+    g, w, before = torch.empty(n, device="cuda"), torch.zeros(n, device="cuda"), torch.tensor([7.0, 7.0, 0.0, 0.0], device="cuda")
+    big = torch.ones(1 << 28, device="cuda")                                     # 1 GiB: a pass over it takes about 0.4 ms
+    norm = gb.GaLoreGradNorm(1, max_norm=1024.0)
+    opt = gb.GaLoreAdamW([w], moments="q8" if call == "step_q8" else "f32", beta1=0.5, beta2=0.75, eps=0.0, capturable=call == "tick")
+    ready = torch.tensor([2048.0, 0.5, 1.0, 0.0], device="cuda")
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        g.fill_(1.0)
+        norm.stats.copy_(before)
+        opt.M_flat.zero_(); opt.V_flat.zero_(); opt.t = 0
+        if opt.clock is not None:
+            opt.clock.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(60):
+                big.mul_(1.0)
+            g.fill_(2.0)
+            if call == "measure":
+                out = norm.measure([g]).clone()
+            elif call == "scale":
+                norm.stats.copy_(ready)
+                norm.scale([g])
+                out = g.clone()
+            elif call == "tick":
+                opt.clock[:8].view(torch.int64).fill_(4)
+                gb.galore_adamw_tick(opt.clock, 0.5, 0.75)
+                out = opt.clock.clone()
+            else:
+                opt.step([w], [g], 0.5)
+                out = torch.cat([(opt.M_scale_flat if call == "step_q8" else opt.M_flat), (opt.V_scale_flat if call == "step_q8" else opt.V_flat)])
+        side.synchronize()
+        if call == "measure":
+            assert out.tolist() == [2048.0, 0.5, 1.0, 0.0]                       # sqrt(4 * 2^20); 1024 / 2048.000001 in fp32
+        elif call == "scale":
+            assert bool((out == 1.0).all())
+        elif call == "tick":
+            assert int(out[:8].view(torch.int64)) == 5
+        else:
+            half = out.numel() // 2
+            assert bool((out[:half] == 1.0).all()) and bool((out[half:] == 1.0).all())    # g / 2 and g^2 / 4
