@@ -1,10 +1,11 @@
 """AdamW over tensor lists, gradient norm and scaling on the GPU at their edges: second moments beyond fp32, memory next to
-the tensors, ends around a workgroup's elements, lists of many workgroups, the stream that the calls go to.
+the tensors, ends around a workgroup's elements, lists of many workgroups, the stream that the calls go to, steps
+that are left out.
 
 Tolerances count roundings (u = 2^-24, half a step of fp32; 2^-8 for a weight stored in bf16).  W = (1 - lr wd) W - lr n: the
 factor of W, its product and the sum are 2u |W| + u |W'|.  n differs from the oracle's by 11u |n| (the oracle rounds m c1, the
 square root, the sum and the quotient: 4u; the step its square root and reciprocal by one unit in the last place, 2u each, and
-lr c1, the sum and a product: 7u); with fp32 moments it is the oracle's own expression, and lr n is rounded: u |lr n|."""
+lr c1, the sum and a product: 7u).  Bounds for fp32 moments stand at their tests."""
 import numpy as np
 import pytest
 import torch
@@ -271,3 +272,33 @@ def test_a_call_waits_for_its_own_stream(call):
         else:
             half = out.numel() // 2
             assert bool((out[:half] == 1.0).all()) and bool((out[half:] == 1.0).all())    # g / 2 and g^2 / 4
+
+
+# ---- steps that are left out -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("moments", ["f32", "q8"])
+def test_hooks_with_the_count_on_the_device_leave_out_steps_that_are_not_finite(moments):
+    # others_options={"capturable": True}: a step whose gradients were not finite neither moves anything nor counts
+    from paper_2403_03507_amd.hooks import PerLayerGaLore
+
+    gen = torch.Generator("cuda").manual_seed(9)
+    fresh = lambda: [torch.randn(s, generator=gen, device="cuda") for s in ((48, 64), (64,), (5, 7))]
+    start = fresh()
+    mat, vec, emb = (torch.nn.Parameter(x.clone()) for x in start)
+    drv = PerLayerGaLore([[mat]], 8, 1e-2, update_gap=100, refresh_iters=3, others=[vec, emb], others_lr=3e-2,
+                         others_options={"moments": moments, "weight_decay": 0.1, "capturable": True})
+    ref_w = [x.clone() for x in start[1:]]
+    ref = gb.GaLoreAdamW(ref_w, moments=moments, weight_decay=0.1)
+    norm, ref_norm = gb.GaLoreGradNorm(2, max_norm=1.0), gb.GaLoreGradNorm(2, max_norm=1.0)
+    for i in range(5):
+        g = fresh()
+        if i in (0, 3):
+            g[2][4, 6] = float("inf")
+        sum((p * x).sum() for p, x in zip((mat, vec, emb), g)).backward()
+        drv.finish(norm.measure([vec.grad, emb.grad]))
+        if i not in (0, 3):
+            ref.step(ref_w, g[1:], 3e-2, ref_norm.measure(g[1:]))
+        torch.cuda.synchronize()
+        assert torch.equal(vec.data, ref_w[0]) and torch.equal(emb.data, ref_w[1]), i
+        assert drv.others_opt.count() == ref.t
+    drv.close()
