@@ -3,7 +3,8 @@
 // Two launches: partial sums of squares per workgroup, then their sum and the square root.  Squares are formed and added
 // in 64 bits: no fp32 or bf16 entry overflows or underflows there, so the sum is finite exactly if every entry is (4
 // instructions per element, a third of what a read at 6.6 TB/s leaves time for).  Bound by HBM: norm of 405M bf16 gradients
-// 123 us (6.6 TB/s), scaling of 151M bf16 93 us (6.5 TB/s); a scaling by 1 of 202M leaves after 22 us, all of it launch.
+// 123 us (6.6 TB/s), scaling of 151M bf16 93 us (6.5 TB/s).  A scaling by 1 moves nothing, but starts its workgroups all the
+// same: 22 us for 202M bf16 gradients, 330 for 3.2 billion.
 #include "adamw.hpp"
 #include "tensor_list.hpp"
 
@@ -18,7 +19,8 @@ constexpr int64_t kOneRoundElements = (int64_t)1 << 26;
 // What follows a norm (AdamW, the scaling) reads the same gradients again and finds a part of them in the 256 MiB cache if
 // they were loaded through it, which the norm itself pays for: norm and AdamW of 25 MB of gradients 53.4 us (loads past the
 // caches 56.1), 240 MB 433 (457), 400 MB 734 (772), 800 MB 1505 (1532), 1600 MB 3046 (3054); the norm alone 76 (67) at 400 MB,
-// 138 (122) at 800.
+// 138 (122) at 800.  The limit serves the pair, and lets go where the norm would pay for little: at 400 MB the pair gains 4
+// times what a norm alone loses (38 us and 9), at 800 MB less than twice (27 and 16).
 constexpr int64_t kCachedBytes = (int64_t)512 << 20;
 constexpr int kScaleThreads = 128;
 // Of a tensor, per workgroup: two 16-byte accesses of every thread (151M bf16 / 200M fp32: 94 / 243 us; one access 113 / 287,

@@ -75,7 +75,8 @@ class PerLayerGaLore:
     def finish(self, stats=None):
         """Call after backward(): steps the other parameters and drops their gradients, and orders the library's
         streams before torch's current stream.  stats: what a `binding.GaLoreGradNorm` measured of the other
-        parameters' gradients (those of the GaLore matrices are gone by now).  Every parameter of `others` needs a
+        parameters' gradients (those of the GaLore matrices are gone by now); where they were not finite nothing of
+        `others` changes, and with others_options={"capturable": True} the step does not count either.  Every parameter of `others` needs a
         gradient: without one ValueError is raised and none of them is stepped.  The streams are ordered also where
         this raises, and the gradients of `others` are kept then."""
         try:

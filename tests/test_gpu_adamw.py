@@ -22,7 +22,7 @@ U, TINY = 2.0 ** -24, 2.0 ** -149
 B1, B2, EPS, LR, WD = f32(0.9), f32(0.999), f32(1e-8), f32(1e-2), f32(0.1)
 STORED = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8}
 
-# one element, less than a vector, vectors and a rest, ends around the spans of a workgroup (2048, 8192) and the blocks of 256
+# one element, less than a vector, vectors and a rest, lengths around powers of two from the blocks of 256 on
 SIZES = [(1, 1), (1, 3), (3, 1), (1, 255), (1, 256), (1, 257), (7, 5), (33, 1023), (2, 1024), (1, 2047), (1, 2049), (64, 129), (5, 8193), (1, 16384)]
 
 
