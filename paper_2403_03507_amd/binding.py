@@ -433,9 +433,13 @@ def galore_grad_norm_workspace_bytes(count):
 
 
 def galore_grad_norm(G, grad_scale, max_norm, stats, workspace):
+    if workspace.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("workspace: need a tensor on the current device")
+    _grad_norm(G, grad_scale, max_norm, stats, workspace)
+
+
+def _grad_norm(G, grad_scale, max_norm, stats, workspace):   # workspace: on the device of stats, which is looked at
     G = _param_array(G)
-    if workspace.get_device() != torch._C._cuda_getDevice() or workspace.dtype != torch.uint8 or workspace.dim() != 1 or workspace.stride(0) != 1:
-        raise ValueError("workspace: contiguous bytes on the current device")
     _check(lib().galore_grad_norm(G, len(G), grad_scale, max_norm, _stats_ptr(stats), workspace.data_ptr(), workspace.numel(), _stream()))
 
 
@@ -455,7 +459,7 @@ class GaLoreGradNorm:
 
     def measure(self, grads, grad_scale=1.0):
         """grads: tensors, or an array of their descriptors (tensor_array(param_desc(g) for g in ...))."""
-        galore_grad_norm(grads, grad_scale, self.max_norm, self.stats, self.workspace)
+        _grad_norm(grads, grad_scale, self.max_norm, self.stats, self.workspace)
         return self.stats
 
     def scale(self, grads, stats=None):
@@ -503,6 +507,7 @@ class GaLoreAdamW:
         self._M_flat, self._V_flat = (torch.zeros(total, dtype=code, device=device) for _ in range(2))
         scales = lambda: torch.zeros(total // self._ALIGN, dtype=torch.float32, device=device) if q8 else None
         self._M_scale_flat, self._V_scale_flat = scales(), scales()
+        self._device = self._M_flat.get_device()
         self._master_flat = torch.zeros(total, dtype=torch.float32, device=device) if master else None
         for i, w in enumerate(weights):
             if self._has_master[i]:
@@ -576,7 +581,7 @@ class GaLoreAdamW:
         step, it is the rate of every replay).  stats: the result of a GaLoreGradNorm; its factor is applied to the
         gradients, and where an entry was not finite nothing changes.  Such a step counts all the same without capturable,
         since the host does not wait for the device to say so: a caller that reads `finite` sets `t` back by one."""
-        if self._places and self.M_flat.get_device() != torch._C._cuda_getDevice():
+        if self._places and self._device != torch._C._cuda_getDevice():
             raise ValueError("the states are on another device than the current one")
         if self.clock is not None:
             if lr is not None:
